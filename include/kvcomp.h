@@ -247,6 +247,87 @@ kvcomp_status kvcomp_baseline_fp16_attn_noalloc(const kvcomp_config *cfg, const 
  * that the loads cannot be optimised away.  Stream-ordered; the caller times it. */
 kvcomp_status kvcomp_probe_read_stream(const void *d_buf, size_t bytes, void *d_sink, size_t *h_bytes_read, void *stream);
 
+/* ---- a paged cache of 8-bit codes for sequences of different lengths --------------------------------------------------
+ * The compressed cache above holds sequences of one length and is read by one query token each.  This one holds sequences
+ * of any lengths in pages of 64 tokens, rotates keys (and queries) on the way in, and is read by single tokens, drafted
+ * tokens and whole prompt chunks.  The calls keep no state in the library: cache, lengths and page tables are the
+ * caller's device memory, and lengths are read on the device, so that a captured step replays with the lengths of the day.
+ * All calls are stream-ordered, launch one kernel each, allocate nothing and never synchronise, except kvcomp_paged_check.
+ * The current device must be the one that the memory is on.
+ *
+ * A block is 64 consecutive tokens of a sequence (tokens 64 j .. 64 j + 63), its page holds it for all KV heads:
+ *   d_k_codes  [n_pages][n_kv_heads][64][head_dim]   one byte a value
+ *   d_v_codes  [n_pages][n_kv_heads][head_dim][64]   one byte a value, channels outermost
+ *   d_scales   fp32 [n_pages][n_kv_heads][2]         of K and of V: a value is code * scale
+ * int8 codes are rne(x * (127 / amax)) with scale = amax / 127, e4m3 codes rne(x * (448 / amax)) with scale = amax / 448,
+ * where amax is the largest magnitude in the block, head and tensor, and all operations are single binary32 ones; a block
+ * with amax < 2^-100 is stored as zeros with scale 0.  Scales are never negative.
+ * The unfinished block of a sequence (its last length % 64 tokens) stays in 16 bits in a tail of its own:
+ *   d_k_tail, d_v_tail  [n_tails][n_kv_heads][64][head_dim]  fp16 or bf16
+ * so what a cache holds does not depend on how its tokens were divided among calls.  A sequence's length may be set back
+ * only within its unfinished block.
+ * Inf or NaN in a new key or value (or a rotated key that overflows fp16) becomes NaN in its token's K and 0 in V: every
+ * output row that sees the token, or the block it ends up in, is NaN, all others are not touched by it. */
+enum { KVCOMP_FP16 = 0, KVCOMP_BF16 = 1 };  /* kvcomp_paged_config.data_type */
+enum { KVCOMP_INT8 = 0, KVCOMP_E4M3 = 1 };  /* kvcomp_paged_config.code_type (e4m3: the OCP format, no infinities) */
+
+typedef struct {
+    int32_t n_kv_heads;
+    int32_t n_q_heads;  /* a multiple of n_kv_heads, at most 32 times it; query head g reads KV head g / (n_q_heads / n_kv_heads) */
+    int32_t head_dim;   /* 64 or 128                                                                         */
+    int32_t data_type;  /* of keys, values, queries, outputs and tails                                       */
+    int32_t code_type;
+    int32_t n_pages;    /* pages and tails that the tensors below have room for                              */
+    int32_t n_tails;
+    int32_t max_pages;  /* entries of a page table row = blocks that a sequence may have, at most 2^20       */
+} kvcomp_paged_config;
+
+typedef struct {        /* DEVICE, caller-owned, 16-byte aligned                                              */
+    void *d_k_codes, *d_v_codes;
+    float *d_scales;
+    void *d_k_tail, *d_v_tail;
+    uint32_t *d_fault;  /* one word that the caller sets to 0 once: what kernels flagged, see kvcomp_paged_check */
+} kvcomp_paged_cache;
+
+typedef struct {        /* the sequences of one call                                                          */
+    int32_t batch;
+    const int32_t *d_lens;   /* DEVICE [batch]: tokens of each sequence, those of this call included; 0 = an empty place */
+    const int32_t *d_table;  /* DEVICE [batch][max_pages]: page of each whole block; the rest is not read.  Sequences may
+                                share pages of whole blocks (they are written once, when the block ends) */
+    const int32_t *d_tails;  /* DEVICE [batch]: tail of each sequence; no two sequences of an append may share one */
+} kvcomp_paged_batch;
+
+typedef struct {        /* the new tokens of one append                                                       */
+    int32_t n_tokens;            /* rows of d_k, d_v, d_q, d_q_out                                              */
+    const int32_t *d_starts;     /* DEVICE [batch + 1]: sequence b appends rows starts[b] .. starts[b+1]-1 (none: equal);
+                                    rows behind starts[batch] take no part.  NULL: one token each, n_tokens = batch, and
+                                    sequences of length 0 take no part */
+    const void *d_k, *d_v;       /* DEVICE [n_tokens][n_kv_heads][head_dim], 16-byte aligned                    */
+    size_t k_stride, v_stride;   /* elements between tokens, multiples of 8                                     */
+    const void *d_q;             /* DEVICE [n_tokens][n_q_heads][head_dim]: queries to rotate along, or NULL    */
+    void *d_q_out;               /* may be d_q (then with its stride)                                           */
+    size_t q_stride, q_out_stride;
+    const float *d_cos_sin;      /* DEVICE fp32 [n_positions][rot_dim]: cosines of the rot_dim / 2 pairs, then their sines;
+                                    NULL: no rotation */
+    int32_t n_positions;
+    int32_t rot_dim;             /* channels that are rotated, a multiple of 16, at most head_dim               */
+    int32_t interleaved;         /* pair p is channels 2p, 2p+1 (1) or p, p + rot_dim/2 (0)                     */
+    int32_t n_axes;              /* 1..3: position axes (time, height, width)                                   */
+    int32_t sections[3];         /* pairs of each axis in order, multiples of 4 that add up to rot_dim / 2      */
+    const int32_t *d_positions;  /* DEVICE [n_axes][n_tokens], or NULL with one axis: a token's place in its sequence */
+} kvcomp_paged_new;
+
+/* Append the new tokens to their sequences: keys (and queries) are rotated, (a, b) -> (a cos - b sin, b cos + a sin) in
+ * binary32 with one rounding to the 16-bit type, blocks that end are quantized into their pages, the rest goes to the
+ * tails.  Errors: INVALID_ARG (shapes, alignment, NULL), HIP. */
+kvcomp_status kvcomp_paged_append(const kvcomp_paged_config *cfg, const kvcomp_paged_cache *cache,
+                                  const kvcomp_paged_batch *seqs, const kvcomp_paged_new *fresh, void *stream);
+
+/* What kernels flagged since the last check, once, and in this order: a page, tail or position out of range, or lengths or
+ * starts that do not fit (STATE: such a sequence's tokens were not stored, its output rows are NaN; a token at a position
+ * outside the table counts as one that holds NaN), Inf or NaN in what was appended (NONFINITE).  SYNCHRONISES `stream` and clears the flags. */
+kvcomp_status kvcomp_paged_check(const kvcomp_paged_cache *cache, void *stream);
+
 const char *kvcomp_last_error(void);
 
 #ifdef __cplusplus

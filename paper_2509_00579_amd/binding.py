@@ -37,9 +37,31 @@ class Stats(C.Structure):
         return {n: getattr(self, n) for n, _ in self._fields_}
 
 
+class PagedConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_kv_heads", "n_q_heads", "head_dim", "data_type", "code_type", "n_pages", "n_tails",
+                                         "max_pages")]
+
+
+class PagedTensors(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("d_k_codes", "d_v_codes", "d_scales", "d_k_tail", "d_v_tail", "d_fault")]
+
+
+class PagedBatch(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("d_lens", C.c_void_p), ("d_table", C.c_void_p), ("d_tails", C.c_void_p)]
+
+
+class PagedNew(C.Structure):
+    _fields_ = [("n_tokens", C.c_int32), ("d_starts", C.c_void_p), ("d_k", C.c_void_p), ("d_v", C.c_void_p),
+                ("k_stride", C.c_size_t), ("v_stride", C.c_size_t), ("d_q", C.c_void_p), ("d_q_out", C.c_void_p),
+                ("q_stride", C.c_size_t), ("q_out_stride", C.c_size_t), ("d_cos_sin", C.c_void_p), ("n_positions", C.c_int32),
+                ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32), ("sections", C.c_int32 * 3),
+                ("d_positions", C.c_void_p)]
+
+
 # every symbol include/kvcomp.h declares: name -> (restype, argtypes)
 _vp, _i, _f = C.c_void_p, C.c_int, C.c_float
 _cfgp = C.POINTER(Config)
+_pcfg, _pmem, _pseq, _pnew = C.POINTER(PagedConfig), C.POINTER(PagedTensors), C.POINTER(PagedBatch), C.POINTER(PagedNew)
 SIGNATURES = {
     "kvcomp_arena_bytes": (C.c_size_t, [_cfgp]),
     "kvcomp_create": (_i, [_cfgp, _vp, C.c_size_t, _vp, C.POINTER(_vp)]),
@@ -68,6 +90,8 @@ SIGNATURES = {
     "kvcomp_baseline_workspace_bytes": (C.c_size_t, [_cfgp]),
     "kvcomp_baseline_fp16_attn": (_i, [_cfgp, _vp, _vp, _i, _vp, _f, _vp, _vp, C.c_size_t, _i, _vp]),
     "kvcomp_baseline_fp16_attn_noalloc": (_i, [_cfgp, _vp, _vp, _i, _vp, _f, _vp, _i, _vp]),
+    "kvcomp_paged_append": (_i, [_pcfg, _pmem, _pseq, _pnew, _vp]),
+    "kvcomp_paged_check": (_i, [_pmem, _vp]),
     "kvcomp_last_error": (C.c_char_p, []),
 }
 
@@ -348,3 +372,123 @@ class BaselineFp16Attention:
                                                           _dev_fp16(q, (self.B, self.Hq, D)), float(scale),
                                                           C.c_void_p(out.data_ptr()), n_splits, _stream()))
         return out
+
+
+class Rope:
+    """The position rotation of PagedCache.append: `cos_sin` is a CUDA fp32 tensor [positions, rot_dim], the cosines of the
+    rot_dim / 2 pairs and then their sines; interleaved: pairs are neighbouring channels instead of the two halves of the
+    rotated ones; sections: pairs per position axis (time, height, width), one axis if None."""
+
+    def __init__(self, cos_sin, interleaved=False, sections=None):
+        assert cos_sin.is_cuda and cos_sin.dtype is torch.float32 and cos_sin.is_contiguous() and cos_sin.dim() == 2
+        self.cos_sin = cos_sin
+        self.n_positions, self.rot_dim = cos_sin.shape
+        sections = [self.rot_dim // 2] if sections is None else list(sections)
+        assert 1 <= len(sections) <= 3, "one to three axes"
+        self.interleaved, self.n_axes = int(interleaved), len(sections)
+        self.sections = (C.c_int32 * 3)(*sections)
+
+    @staticmethod
+    def table(n_positions, rot_dim, base=10000.0, device="cuda:0"):
+        """The usual table: the angle of pair p at position n is n * base^(-2p / rot_dim), taken in 64 bits."""
+        half = rot_dim // 2
+        angle = torch.arange(n_positions, device=device, dtype=torch.float64)[:, None] * base ** (
+            -torch.arange(half, device=device, dtype=torch.float64) / half)
+        return torch.cat([angle.cos(), angle.sin()], dim=1).float()
+
+
+class PagedCache:
+    """One layer's paged KV cache of 8-bit codes for sequences of different lengths (the layout stands in include/kvcomp.h).
+
+    The pages, scales and tails are tensors of the caller's, `storage` = (k_codes, v_codes, scales, k_tail, v_tail), or are
+    allocated here.  Which sequence has which pages and tail, and how long it is, comes with every call: lens [batch], table
+    [batch, max_pages] and tails [batch] are int32 CUDA tensors, read on the device.  lens counts the call's own tokens.
+    Calls on one cache from several streams at a time need a workspace each (new_workspace)."""
+
+    def __init__(self, n_kv_heads, n_q_heads, n_pages, n_tails, head_dim=D, dtype=torch.float16, codes="int8", device="cuda:0",
+                 storage=None):
+        self.lib = load()
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.H, self.Hq, self.D, self.dtype = n_kv_heads, n_q_heads, head_dim, dtype
+        self.n_pages, self.n_tails = n_pages, n_tails
+        code = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}[codes]
+        kinds = (("k_codes", (n_pages, n_kv_heads, BT, head_dim), code), ("v_codes", (n_pages, n_kv_heads, head_dim, BT), code),
+                 ("scales", (n_pages, n_kv_heads, 2), torch.float32), ("k_tail", (n_tails, n_kv_heads, BT, head_dim), dtype),
+                 ("v_tail", (n_tails, n_kv_heads, BT, head_dim), dtype))
+        if storage is None:
+            storage = [torch.empty(shape, dtype=t, device=self.device) for _, shape, t in kinds]
+        for (name, shape, t), x in zip(kinds, storage):
+            assert x.device == self.device and x.dtype is t and x.is_contiguous() and x.shape == shape, (
+                f"{name} must be a contiguous {t} tensor {shape} on {self.device}")
+            setattr(self, name, x)
+        self.fault = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._types = (head_dim, {torch.float16: 0, torch.bfloat16: 1}[dtype], int(codes == "e4m3"), n_pages, n_tails)
+        self._memory = PagedTensors(*(x.data_ptr() for x in (*storage, self.fault)))
+        self._config = {}
+
+    def _cfg(self, max_pages):
+        cfg = self._config.get(max_pages)
+        if cfg is None:
+            cfg = self._config[max_pages] = PagedConfig(self.H, self.Hq, *self._types, max_pages)
+        return cfg
+
+    def _batch(self, lens, table, tails):
+        i32, dev = torch.int32, self.device
+        n = lens.shape[0]
+        assert lens.dtype is i32 and table.dtype is i32 and tails.dtype is i32, "lens, table and tails are int32"
+        assert lens.device == dev and table.device == dev and tails.device == dev, f"lens, table and tails must be on {dev}"
+        assert table.dim() == 2 and table.shape[0] == n and tails.shape == (n,) and lens.dim() == 1, "one row per sequence"
+        assert table.is_contiguous() and lens.is_contiguous() and tails.is_contiguous(), "lens, table and tails must be contiguous"
+        return PagedBatch(n, lens.data_ptr(), table.data_ptr(), tails.data_ptr())
+
+    def _rows(self, x, n, heads, name):
+        """Pointer and token stride of a tensor [n, heads, head_dim] whose tokens may be apart (a slice of a fused projection)."""
+        assert x.device == self.device and x.dtype is self.dtype, f"{name} must be {self.dtype} on {self.device}"
+        assert x.shape == (n, heads, self.D), f"{name}: expected shape {(n, heads, self.D)}, got {tuple(x.shape)}"
+        s = x.stride()
+        assert s[2] == 1 and (s[1] == self.D or heads == 1), f"the heads of a token of {name} must be contiguous"
+        return x.data_ptr(), s[0] if n > 1 else heads * self.D
+
+    def _on_device(self):
+        if torch._C._cuda_getDevice() != self.device.index:
+            raise KvcompError(ERR_INVALID_ARG, f"the current device is not the cache's ({self.device})")
+        return torch._C._cuda_getCurrentRawStream(self.device.index)
+
+    def append(self, k, v, lens, table, tails, starts=None, q=None, q_out=None, rope=None, positions=None):
+        """Append k, v [n, n_kv_heads, head_dim]: one token per sequence (starts None: n = batch), or rows starts[b] ..
+        starts[b + 1] to sequence b (starts: int32 [batch + 1]).  With `rope`, keys are rotated, and queries q into q_out (which
+        may be q, and is q's rotated copy if None) with them; positions: int32 [axes, n] (default: a token's place).
+        Returns q_out."""
+        stream = self._on_device()
+        n = k.shape[0]
+        seqs = self._batch(lens, table, tails)
+        kp, ks = self._rows(k, n, self.H, "k")
+        vp, vs = self._rows(v, n, self.H, "v")
+        sp = qp = qs = op = os_ = cp = n_pos = rot = inter = pp = 0
+        axes, sections = 1, (C.c_int32 * 3)()
+        if starts is not None:
+            assert starts.dtype is torch.int32 and starts.device == self.device and starts.is_contiguous()
+            assert starts.shape == (lens.shape[0] + 1,), "starts: one entry per sequence and the end"
+            sp = starts.data_ptr()
+        if q is not None:
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            qp, qs = self._rows(q, n, self.Hq, "q")
+            op, os_ = self._rows(q_out, n, self.Hq, "q_out")
+        if rope is not None:
+            assert rope.cos_sin.device == self.device
+            cp, n_pos, rot, inter, axes, sections = (rope.cos_sin.data_ptr(), rope.n_positions, rope.rot_dim, rope.interleaved,
+                                                     rope.n_axes, rope.sections)
+            if positions is not None:
+                assert positions.dtype is torch.int32 and positions.device == self.device and positions.is_contiguous()
+                assert positions.shape == (axes, n), f"positions: expected shape {(axes, n)}, got {tuple(positions.shape)}"
+                pp = positions.data_ptr()
+        new = PagedNew(n, sp, kp, vp, ks, vs, qp, op, qs, os_, cp, n_pos, rot, inter, axes, sections, pp)
+        _check(self.lib.kvcomp_paged_append(self._cfg(table.shape[1]), self._memory, seqs, new, stream))
+        return q_out
+
+    def check(self):
+        """Raises what kernels flagged since the last check (pages out of range, Inf or NaN appended); synchronises."""
+        _check(self.lib.kvcomp_paged_check(self._memory, self._on_device()))

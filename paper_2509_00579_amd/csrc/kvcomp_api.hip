@@ -10,31 +10,22 @@
 #include <vector>
 
 #include "../../include/kvcomp.h"
+#include "api_error.h"
 #include "host_logic.h"
 #include "kvcomp_internal.h"
 
 using namespace kvc;
 using namespace kvc::host;
 
-namespace {
+static thread_local char g_err[512] = "";
 
-thread_local char g_err[512] = "";
-
-kvcomp_status fail(kvcomp_status st, const char *fmt, ...) {
+kvcomp_status kvc::fail(kvcomp_status st, const char *fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
     vsnprintf(g_err, sizeof(g_err), fmt, ap);
     va_end(ap);
     return st;
 }
-
-#define HIP_TRY(expr)                                                                              \
-    do {                                                                                           \
-        hipError_t e_ = (expr);                                                                    \
-        if (e_ != hipSuccess) return fail(KVCOMP_ERR_HIP, "%s: %s", #expr, hipGetErrorString(e_)); \
-    } while (0)
-
-}  // namespace
 
 struct kvcomp_ctx {
     kvcomp_config cfg;

@@ -1,0 +1,136 @@
+// The C entry points of the paged cache of 8-bit codes: checks of what the host can see, and the launches.
+#include "api_error.h"
+#include "paged.cuh"
+
+using namespace kvc;
+
+namespace {
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+constexpr int kMaxGroup = 32, kMaxPagesPerSeq = 1 << 20;
+
+kvcomp_status check_config(const kvcomp_paged_config *c) {
+    if (!c) return fail(KVCOMP_ERR_INVALID_ARG, "NULL argument");
+    if (c->n_kv_heads < 1 || c->n_q_heads < 1 || c->n_q_heads % c->n_kv_heads || c->n_q_heads / c->n_kv_heads > kMaxGroup)
+        return fail(KVCOMP_ERR_INVALID_ARG, "n_q_heads must be 1 to %d times n_kv_heads", kMaxGroup);
+    if (c->head_dim != 64 && c->head_dim != 128) return fail(KVCOMP_ERR_INVALID_ARG, "head_dim must be 64 or 128");
+    if (c->data_type != KVCOMP_FP16 && c->data_type != KVCOMP_BF16) return fail(KVCOMP_ERR_INVALID_ARG, "unknown data_type");
+    if (c->code_type != KVCOMP_INT8 && c->code_type != KVCOMP_E4M3) return fail(KVCOMP_ERR_INVALID_ARG, "unknown code_type");
+    if (c->n_pages < 1 || c->n_tails < 1) return fail(KVCOMP_ERR_INVALID_ARG, "n_pages and n_tails must be positive");
+    if (c->max_pages < 1 || c->max_pages > kMaxPagesPerSeq)
+        return fail(KVCOMP_ERR_INVALID_ARG, "max_pages must be 1 to %d", kMaxPagesPerSeq);
+    return KVCOMP_OK;
+}
+
+kvcomp_status check_all(const kvcomp_paged_config *c, const kvcomp_paged_cache *m, const kvcomp_paged_batch *b, PagedGeo *g) {
+    kvcomp_status st = check_config(c);
+    if (st) return st;
+    if (!m || !b || !m->d_k_codes || !m->d_v_codes || !m->d_scales || !m->d_k_tail || !m->d_v_tail || !m->d_fault)
+        return fail(KVCOMP_ERR_INVALID_ARG, "NULL argument");
+    if (!aligned16(m->d_k_codes) || !aligned16(m->d_v_codes) || !aligned16(m->d_scales) || !aligned16(m->d_k_tail) ||
+        !aligned16(m->d_v_tail) || (reinterpret_cast<uintptr_t>(m->d_fault) & 3u))
+        return fail(KVCOMP_ERR_INVALID_ARG, "the cache's tensors must be 16-byte aligned");
+    if (b->batch < 0 || (b->batch && (!b->d_lens || !b->d_table || !b->d_tails))) return fail(KVCOMP_ERR_INVALID_ARG, "bad batch");
+    if ((long long)b->batch * c->n_q_heads > (1ll << 24)) return fail(KVCOMP_ERR_INVALID_ARG, "more than 2^24 sequences times query heads");
+    g->H = c->n_kv_heads;
+    g->G = c->n_q_heads / c->n_kv_heads;
+    g->n_pages = c->n_pages;
+    g->n_tails = c->n_tails;
+    g->max_pages = c->max_pages;
+    g->batch = b->batch;
+    g->k_codes = static_cast<uint8_t *>(m->d_k_codes);
+    g->v_codes = static_cast<uint8_t *>(m->d_v_codes);
+    g->scales = m->d_scales;
+    g->k_tail = static_cast<uint16_t *>(m->d_k_tail);
+    g->v_tail = static_cast<uint16_t *>(m->d_v_tail);
+    g->fault = m->d_fault;
+    g->lens = b->d_lens;
+    g->table = b->d_table;
+    g->tails = b->d_tails;
+    return KVCOMP_OK;
+}
+
+// a tensor of rows [n][heads][head_dim] with `stride` elements from row to row
+kvcomp_status check_rows(const char *name, const void *p, size_t stride, int heads, int head_dim) {
+    if (!p) return fail(KVCOMP_ERR_INVALID_ARG, "%s is NULL", name);
+    if (!aligned16(p) || stride % 8) return fail(KVCOMP_ERR_INVALID_ARG, "rows of %s must start at multiples of 16 bytes", name);
+    if (stride < (size_t)heads * head_dim) return fail(KVCOMP_ERR_INVALID_ARG, "rows of %s overlap", name);
+    return KVCOMP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+kvcomp_status kvcomp_paged_append(const kvcomp_paged_config *cfg, const kvcomp_paged_cache *cache,
+                                  const kvcomp_paged_batch *seqs, const kvcomp_paged_new *fresh, void *stream) {
+    PagedGeo g;
+    kvcomp_status st = check_all(cfg, cache, seqs, &g);
+    if (st) return st;
+    if (!fresh) return fail(KVCOMP_ERR_INVALID_ARG, "NULL argument");
+    const kvcomp_paged_new &f = *fresh;
+    if (f.n_tokens < 0) return fail(KVCOMP_ERR_INVALID_ARG, "n_tokens is negative");
+    if (!f.d_starts && f.n_tokens != g.batch) return fail(KVCOMP_ERR_INVALID_ARG, "without d_starts there is one token per sequence");
+    if ((long long)f.n_tokens * cfg->n_q_heads > (1ll << 30)) return fail(KVCOMP_ERR_INVALID_ARG, "more than 2^30 tokens times query heads");
+    PagedNew n = {};
+    n.rot_dim = 0;
+    if (f.d_cos_sin) {
+        if (f.rot_dim < 16 || f.rot_dim % 16 || f.rot_dim > cfg->head_dim)
+            return fail(KVCOMP_ERR_INVALID_ARG, "rot_dim must be a multiple of 16, at most head_dim");
+        if (!aligned16(f.d_cos_sin) || f.n_positions < 1) return fail(KVCOMP_ERR_INVALID_ARG, "d_cos_sin must be 16-byte aligned and hold a position");
+        if (f.n_axes < 1 || f.n_axes > 3 || (f.n_axes > 1 && !f.d_positions))
+            return fail(KVCOMP_ERR_INVALID_ARG, "n_axes must be 1 to 3, and several axes need positions");
+        int sum = 0;
+        for (int a = 0; a < f.n_axes; a++) {
+            if (f.sections[a] < 0 || f.sections[a] % 4) return fail(KVCOMP_ERR_INVALID_ARG, "sections must be multiples of 4");
+            sum += f.sections[a];
+            if (a < 2) n.edge[a] = sum;
+        }
+        if (sum != f.rot_dim / 2) return fail(KVCOMP_ERR_INVALID_ARG, "sections must add up to rot_dim / 2");
+        for (int a = f.n_axes - 1; a < 2; a++) n.edge[a] = 1 << 20;  // no such axis
+        n.rot_dim = f.rot_dim;
+        n.cos_sin = f.d_cos_sin;
+        n.positions = f.d_positions;
+        n.n_positions = f.n_positions;
+        n.interleaved = f.interleaved != 0;
+    }
+    if (!g.batch || !f.n_tokens) return KVCOMP_OK;
+    if ((st = check_rows("d_k", f.d_k, f.k_stride, cfg->n_kv_heads, cfg->head_dim))) return st;
+    if ((st = check_rows("d_v", f.d_v, f.v_stride, cfg->n_kv_heads, cfg->head_dim))) return st;
+    if (f.d_q || f.d_q_out) {
+        if ((st = check_rows("d_q", f.d_q, f.q_stride, cfg->n_q_heads, cfg->head_dim))) return st;
+        if ((st = check_rows("d_q_out", f.d_q_out, f.q_out_stride, cfg->n_q_heads, cfg->head_dim))) return st;
+        if (f.d_q == f.d_q_out && f.q_stride != f.q_out_stride) return fail(KVCOMP_ERR_INVALID_ARG, "queries in place with another stride");
+    }
+    n.n_tokens = f.n_tokens;
+    n.starts = f.d_starts;
+    n.k = static_cast<const uint16_t *>(f.d_k);
+    n.v = static_cast<const uint16_t *>(f.d_v);
+    n.q = static_cast<const uint16_t *>(f.d_q);
+    n.q_out = static_cast<uint16_t *>(f.d_q_out);
+    n.k_stride = f.k_stride;
+    n.v_stride = f.v_stride;
+    n.q_stride = f.q_stride;
+    n.q_out_stride = f.q_out_stride;
+    HIP_TRY(launch_paged_append(g, n, cfg->head_dim, cfg->data_type, cfg->code_type, static_cast<hipStream_t>(stream)));
+    return KVCOMP_OK;
+}
+
+kvcomp_status kvcomp_paged_check(const kvcomp_paged_cache *cache, void *stream) {
+    if (!cache || !cache->d_fault) return fail(KVCOMP_ERR_INVALID_ARG, "NULL argument");
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    uint32_t fault = 0;
+    HIP_TRY(hipMemcpyAsync(&fault, cache->d_fault, sizeof(fault), hipMemcpyDeviceToHost, s));
+    HIP_TRY(hipStreamSynchronize(s));
+    if (!fault) return KVCOMP_OK;
+    HIP_TRY(hipMemsetAsync(cache->d_fault, 0, sizeof(fault), s));
+    HIP_TRY(hipStreamSynchronize(s));
+    if (fault & kFaultPage) return fail(KVCOMP_ERR_STATE, "a page that was needed is outside the cache");
+    if (fault & kFaultTail) return fail(KVCOMP_ERR_STATE, "a tail that was needed is outside the cache");
+    if (fault & kFaultLength) return fail(KVCOMP_ERR_STATE, "a length or a start does not fit");
+    if (fault & kFaultPosition) return fail(KVCOMP_ERR_STATE, "a position is outside the table of cosines and sines");
+    return fail(KVCOMP_ERR_NONFINITE, "an appended token held Inf or NaN");
+}
+
+}  // extern "C"

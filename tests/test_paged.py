@@ -1,0 +1,310 @@
+"""The operators of the paged 8-bit cache on the GPU, against the plain model in 64 bits of paged_model.py."""
+import itertools
+import math
+import random
+
+import pytest
+import torch
+
+import paged_model as M
+
+pytestmark = pytest.mark.gpu
+BT = 64
+TYPES = [(torch.float16, "int8"), (torch.float16, "e4m3"), (torch.bfloat16, "int8"), (torch.bfloat16, "e4m3")]
+IDS = ["fp16-int8", "fp16-e4m3", "bf16-int8", "bf16-e4m3"]
+
+
+@pytest.fixture(scope="module")
+def gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2509_00579_amd import binding
+    binding.load()
+    return binding
+
+
+def _i32(x):
+    return torch.as_tensor(x, dtype=torch.int32, device="cuda:0")
+
+
+class World:
+    """A cache with sequences in it: appends go to the GPU and into the model."""
+
+    def __init__(self, gpu, batch, H, G, D, dtype, codes, max_pages, seed=0, garbage=True):
+        self.gen = torch.Generator().manual_seed(seed)
+        self.batch, self.H, self.Hq, self.D, self.dtype = batch, H, H * G, D, dtype
+        n_pages = batch * max_pages + 2
+        self.cache = gpu.PagedCache(H, H * G, n_pages, batch + 1, head_dim=D, dtype=dtype, codes=codes)
+        if garbage:  # what is not written yet is never looked at
+            self.cache.k_tail.fill_(math.nan)
+            self.cache.v_tail.fill_(math.nan)
+            self.cache.scales.fill_(math.nan)
+        self.table = torch.randperm(n_pages, generator=self.gen)[:batch * max_pages].view(batch, max_pages)
+        self.tails = torch.randperm(batch + 1, generator=self.gen)[:batch]
+        self.d_table, self.d_tails = _i32(self.table), _i32(self.tails)
+        self.seqs, self.lens = M.Sequences(batch), [0] * batch
+        self.scale_c = torch.exp(0.5 * torch.randn((H, D), generator=self.gen, dtype=torch.float64))
+        self.scale_c[:, :2] *= 10
+
+    def rand(self, *shape):
+        return torch.randn(shape, generator=self.gen, dtype=torch.float64)
+
+    def tokens(self, n):
+        k = (self.rand(n, self.H, self.D) * self.scale_c).to(self.dtype)
+        return k, self.rand(n, self.H, self.D).to(self.dtype), self.rand(n, self.Hq, self.D).to(self.dtype)
+
+    def append(self, counts, k, v, q=None, rope=None, positions=None, starts=True, **kw):
+        """counts[b] new tokens of every sequence, rows of k, v, q one after the other."""
+        n = sum(counts)
+        seq = [b for b, c in enumerate(counts) for _ in range(c)]
+        place = [self.lens[b] + i for b, c in enumerate(counts) for i in range(c)]
+        self.lens = [a + c for a, c in zip(self.lens, counts)]
+        args = dict(rope=None, positions=None)
+        pos = torch.tensor(place)[None] if positions is None else positions
+        if rope is not None:
+            cos_sin, inter, sections, binding = rope
+            args["rope"] = binding.Rope(cos_sin.cuda(), inter, sections)
+            if positions is not None:
+                args["positions"] = _i32(positions)
+            kr, size = M.rotate(k[:n].double(), cos_sin, pos, inter, sections)
+        else:
+            kr, size = k[:n].double(), torch.zeros_like(k[:n], dtype=torch.float64)
+        for i in range(n):
+            self.seqs.add(seq[i], [kr[i]], [size[i]], [v[i].double()])
+        if starts:
+            args["starts"] = _i32(list(itertools.accumulate([0] + list(counts))))
+        got = self.cache.append(k.cuda(), v.cuda(), _i32(self.lens), self.d_table, self.d_tails,
+                                q=None if q is None else q.cuda(), **args, **kw)
+        if q is not None:
+            want, size = M.rotate(q[:n].double(), rope[0], pos, rope[1], rope[2]) if rope else (q[:n].double(), 0 * q[:n].double())
+            slack = 3 * 2.0 ** -24 * size
+            tol = slack + torch.finfo(self.dtype).eps / 2 * (want.abs() + slack) + (2.0 ** -25 if self.dtype is torch.float16 else 0)
+            err = (got[:n].cpu().double() - want).abs()
+            assert bool((err <= tol).all()), float((err - tol).max())
+        return got
+
+    def check(self):
+        torch.cuda.synchronize()
+        self.cache.check()
+        M.check_stored(self.cache, self.seqs, self.table, self.tails, self.lens)
+
+
+@pytest.mark.parametrize("dtype,codes", TYPES, ids=IDS)
+@pytest.mark.parametrize("H,G,D", [(1, 1, 128), (3, 4, 64), (8, 2, 128)])
+def test_append_chunks(gpu, dtype, codes, H, G, D):
+    """Ragged chunks, empty ones, chunks that end a block exactly, that begin and end inside blocks, that span several."""
+    w = World(gpu, 5, H, G, D, dtype, codes, 8, seed=H + D)
+    cos_sin = gpu.Rope.table(600, D).cpu()
+    for counts in ([1, 64, 0, 63, 130], [62, 1, 0, 1, 200], [0, 70, 5, 64, 2], [1, 0, 59, 128, 1], [130, 129, 128, 127, 0]):
+        k, v, q = w.tokens(sum(counts))
+        w.append(counts, k, v, q, rope=(cos_sin, False, None, gpu))
+        w.check()
+
+
+@pytest.mark.parametrize("dtype,codes", TYPES, ids=IDS)
+def test_append_single_tokens(gpu, dtype, codes):
+    """One token per sequence, through the ends of two blocks."""
+    w = World(gpu, 3, 2, 3, 64, dtype, codes, 4, seed=5)
+    cos_sin = gpu.Rope.table(200, 32).cpu()
+    k, v, q = w.tokens(100)
+    w.append([61, 0, 39], k, v, q, rope=(cos_sin, True, None, gpu))
+    for i in range(70):
+        k, v, q = w.tokens(3)
+        w.append([1, 1, 1], k, v, q, rope=(cos_sin, True, None, gpu), starts=False)
+        if i in (0, 1, 2, 3, 24, 25, 63, 64, 69):
+            w.check()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("D,rot,sections", [(128, 128, [16, 24, 24]), (128, 64, [4, 12, 16]), (64, 32, [8, 8]), (64, 64, [32]), (128, 16, [8])])
+def test_append_positions_with_axes(gpu, D, rot, sections, interleaved):
+    w = World(gpu, 2, 2, 1, D, torch.float16, "int8", 4, seed=rot)
+    cos_sin = gpu.Rope.table(5000, rot, base=1e6).cpu()
+    for counts in ([70, 3], [1, 128]):
+        k, v, q = w.tokens(sum(counts))
+        pos = torch.randint(0, 5000, (len(sections), sum(counts)), generator=w.gen)
+        pos[0, 0], pos[-1, -1] = 4999, 0
+        w.append(counts, k, v, q, rope=(cos_sin, interleaved, sections, gpu), positions=pos)
+        w.check()
+
+
+@pytest.mark.parametrize("dtype,codes", TYPES, ids=IDS)
+def test_append_does_not_depend_on_the_division_into_calls(gpu, dtype, codes):
+    """The same tokens at once, in chunks and one by one leave the same bits."""
+    counts, states = [150, 64, 7], []
+    cos_sin = gpu.Rope.table(200, 128)
+    for way in (0, 1, 2):
+        w = World(gpu, 3, 2, 2, 128, dtype, codes, 4, seed=9, garbage=False)
+        for t in (w.cache.k_codes, w.cache.v_codes):
+            t.view(torch.uint8).zero_()
+        for t in (w.cache.scales, w.cache.k_tail, w.cache.v_tail):
+            t.zero_()
+        k, v, q = (x.cuda() for x in w.tokens(sum(counts)))
+        first = [0, 150, 214]
+        lens = [0, 0, 0]
+        cuts = {0: [[150, 64, 7]], 1: [[1, 63, 7], [100, 1, 0], [49, 0, 0]], 2: [[1, 1, 1]] * 7 + [[1, 1, 0]] * 57 + [[1, 0, 0]] * 86}[way]
+        for c in cuts:
+            rows = torch.cat([torch.arange(first[b] + lens[b], first[b] + lens[b] + c[b]) for b in range(3)]).cuda()
+            lens = [a + x for a, x in zip(lens, c)]
+            w.cache.append(k[rows], v[rows], _i32(lens), w.d_table, w.d_tails, rope=gpu.Rope(cos_sin),
+                           starts=_i32([0, c[0], c[0] + c[1], sum(c)]))
+        assert lens == counts
+        n = [x % BT for x in counts]
+        tails = [t[int(w.tails[b]), :, :n[b]].clone() for b in range(3) for t in (w.cache.k_tail, w.cache.v_tail)]
+        states.append([w.cache.k_codes.view(torch.uint8), w.cache.v_codes.view(torch.uint8), w.cache.scales, *tails])
+    for other in states[1:]:
+        for a, b in zip(states[0], other):
+            assert torch.equal(a, b)
+
+
+def test_append_strided_rows_in_place_queries_and_rows_behind_the_end(gpu):
+    """Slices of a fused projection; queries rotated in place; rows behind the last sequence are left as they were."""
+    H, G, D, n = 2, 3, 64, 90
+    w = World(gpu, 2, H, G, D, torch.bfloat16, "int8", 4, seed=3)
+    cos_sin = gpu.Rope.table(100, 64)
+    k, v, q = w.tokens(n + 6)
+    fused = torch.cat([x.flatten(1) for x in (q, k, v)], dim=1).cuda()
+    dq, dk, dv = (x.unflatten(1, (-1, D)) for x in fused.split([H * G * D, H * D, H * D], dim=1))
+    starts = _i32([0, 65, 90])
+    want = w.cache.append(k.cuda(), v.cuda(), _i32([65, 25]), w.d_table, w.d_tails, starts=starts, q=q.cuda(), rope=gpu.Rope(cos_sin),
+                          q_out=torch.zeros_like(q, device="cuda:0"))
+    assert torch.equal(want[90:], torch.zeros_like(want[90:]))
+    state = [x.clone() for x in (w.cache.k_codes, w.cache.v_codes, w.cache.scales[w.table[0, 0]], w.cache.k_tail[:, :, :1])]
+    page = int(w.table[0, 0])
+    for t in (w.cache.k_codes, w.cache.v_codes):
+        t[page] = 0
+    w.cache.append(dk, dv, _i32([65, 25]), w.d_table, w.d_tails, starts=starts, q=dq, q_out=dq, rope=gpu.Rope(cos_sin))
+    now = [w.cache.k_codes, w.cache.v_codes, w.cache.scales[w.table[0, 0]], w.cache.k_tail[:, :, :1]]
+    for a, b in zip(state[2:], now[2:]):
+        assert torch.equal(a.nan_to_num(7.), b.nan_to_num(7.))
+    assert torch.equal(state[0][page], now[0][page]) and torch.equal(state[1][page], now[1][page])
+    assert torch.equal(dq[:90], want[:90]) and torch.equal(dq[90:].cpu(), q[90:])
+    assert torch.equal(dk.cpu(), k) and torch.equal(dv.cpu(), v)
+
+
+@pytest.mark.parametrize("dtype,codes", TYPES, ids=IDS)
+def test_append_small_zero_and_large_values(gpu, dtype, codes):
+    """Blocks of zeros, of values near the smallest and the largest of the type, of one value among zeros."""
+    w = World(gpu, 4, 2, 1, 64, dtype, codes, 2, seed=1)
+    k, v, _ = w.tokens(4 * 64)
+    big = torch.finfo(dtype).max
+    k[:64], v[:64] = 0, 0
+    k[64:128] = (k[64:128].double() * (2.0 ** -22 if dtype is torch.float16 else 2.0 ** -126)).to(dtype)
+    v[64:128] = (v[64:128].double() * (2.0 ** -22 if dtype is torch.float16 else 2.0 ** -104)).to(dtype)
+    k[128:192], v[128:192] = k[128:192].sign() * big, -v[128:192].sign() * big
+    k[192:], v[192:] = 0, 0
+    k[200, 1, 5], v[255, 0, 63] = -3, 1.5
+    w.append([64, 64, 64, 64], k, v)
+    w.check()
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_append_reports_non_finite_values(gpu, bad):
+    """Noticed by the check; NaN in K and 0 in V of that token, a block with such a token has a NaN scale for K; once reported."""
+    for which, starts in itertools.product("kv", (True, False)):
+        w = World(gpu, 2, 2, 1, 128, torch.float16, "int8", 2, seed=2)
+        k, v, _ = w.tokens(64 + 63)
+        (k if which == "k" else v)[64 + 3, 1, 40] = bad
+        w.append([64, 63], k, v)
+        with pytest.raises(gpu.KvcompError) as e:
+            w.cache.check()
+        assert e.value.status == gpu.ERR_NONFINITE
+        w.cache.check()
+        t = int(w.tails[1])
+        assert torch.isnan(w.cache.k_tail[t, 1, 3]).any() and torch.isfinite(w.cache.k_tail[t, 0, :63]).all()
+        assert torch.isfinite(w.cache.v_tail[t, :, :63]).all()
+        k, v, _ = w.tokens(2)
+        w.append([1, 1], k, v, starts=starts)
+        w.cache.check()  # the new tokens are finite
+        s = w.cache.scales[int(w.table[1, 0])]
+        assert torch.isnan(s[1, 0]) and torch.isfinite(s[0]).all() and torch.isfinite(s[1, 1])
+        assert torch.isfinite(w.cache.scales[int(w.table[0, 0])]).all()
+
+
+def test_append_refuses_on_the_device_what_only_it_sees(gpu):
+    """Pages, tails, lengths, starts and positions out of range: nothing is stored for such a sequence, the others are, and the
+    check says so once."""
+    def fresh():
+        w = World(gpu, 3, 2, 1, 64, torch.float16, "int8", 2, seed=4)
+        return w, *(x.cuda() for x in w.tokens(3 * 64)[:2])
+
+    rope = gpu.Rope(gpu.Rope.table(64, 64))
+    for what in ("page", "page_low", "tail", "length", "length_low", "starts", "starts_end", "more_than_length", "position"):
+        w, k, v = fresh()
+        lens, table, tails, starts, args = [64, 64, 64], w.table.clone(), w.tails.clone(), [0, 64, 128, 192], {}
+        if what == "page":
+            table[1, 0] = w.cache.n_pages
+        elif what == "page_low":
+            table[1, 0] = -1
+        elif what == "tail":
+            tails[1] = w.cache.n_tails
+        elif what == "length":
+            lens[1] = 129
+        elif what == "length_low":
+            lens[1], starts = -5, [0, 64, 64, 128]
+        elif what == "starts":
+            starts = [0, 64, 60, 124]
+        elif what == "starts_end":
+            starts, lens = [0, 64, 64, 193], [64, 0, 128]
+        elif what == "more_than_length":
+            lens[1] = 63
+        else:
+            pos = torch.arange(192) % 64
+            pos[70] = 64
+            args = dict(rope=rope, positions=_i32(pos[None]))
+        before = [x.clone() for x in (w.cache.scales, w.cache.k_tail, w.cache.v_tail)]
+        w.cache.append(k, v, _i32(lens), _i32(table), _i32(tails), starts=_i32(starts), **args)
+        with pytest.raises(gpu.KvcompError) as e:
+            w.cache.check()
+        assert e.value.status == gpu.ERR_STATE, what
+        w.cache.check()
+        assert torch.isfinite(w.cache.scales[int(w.table[0, 0])]).all(), what
+        own = w.cache.scales[int(w.table[2 if what == "starts_end" else 1, 0])]
+        assert torch.isnan(own[:, 0]).all(), what  # as it was, or a NaN for the position
+        for a, b in zip(before[1:], (w.cache.k_tail, w.cache.v_tail)):
+            assert torch.equal(a.nan_to_num(3.), b.nan_to_num(3.)), what
+
+
+def test_append_single_token_out_of_range(gpu):
+    w = World(gpu, 3, 1, 1, 64, torch.float16, "e4m3", 1, seed=8)
+    k, v, q = (x.cuda() for x in w.tokens(3))
+    out = torch.zeros_like(q)
+    w.cache.append(k, v, _i32([65, 0, 1]), w.d_table, w.d_tails, q=q, q_out=out, rope=gpu.Rope(gpu.Rope.table(64, 64)))
+    with pytest.raises(gpu.KvcompError) as e:
+        w.cache.check()
+    assert e.value.status == gpu.ERR_STATE
+    assert torch.isnan(out[0]).any() and torch.equal(out[1], torch.zeros_like(out[1])) and torch.equal(out[2], q[2])
+    tails = [int(t) for t in w.tails]
+    assert torch.isnan(w.cache.k_tail[tails[0]]).all() and torch.isnan(w.cache.k_tail[tails[1]]).all()
+    assert torch.equal(w.cache.k_tail[tails[2], :, 0], k[2])
+
+
+def test_append_captured_and_replayed(gpu):
+    """A captured step replays with the lengths of the day: the graph advances them."""
+    w = World(gpu, 2, 2, 2, 128, torch.float16, "int8", 3, seed=6)
+    k, v, q = w.tokens(62 + 20)
+    rope = gpu.Rope(gpu.Rope.table(200, 128))
+    w.append([62, 20], k, v, q, rope=(rope.cos_sin.cpu(), False, None, gpu))
+    lens, one = _i32(w.lens), _i32([1, 1])
+    dk, dv, dq = (torch.empty_like(x[:2], device="cuda:0") for x in (k, v, q))
+    out = torch.empty_like(dq)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        lens.add_(one)
+        w.cache.append(dk, dv, lens, w.d_table, w.d_tails, q=dq, q_out=out, rope=rope)
+    for _ in range(5):
+        k, v, q = w.tokens(2)
+        pos = torch.tensor([w.lens])
+        w.lens = [x + 1 for x in w.lens]
+        kr, size = M.rotate(k.double(), rope.cos_sin.cpu(), pos)
+        for b in range(2):
+            w.seqs.add(b, [kr[b]], [size[b]], [v[b].double()])
+        for a, b in ((dk, k), (dv, v), (dq, q)):
+            a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        want, size = M.rotate(q.double(), rope.cos_sin.cpu(), pos)
+        assert bool(((out.cpu().double() - want).abs() <= 3 * 2.0 ** -24 * size + 2.0 ** -11 * want.abs() * 1.001 + 2.0 ** -25).all())
+        w.check()

@@ -1,0 +1,101 @@
+"""What the paged cache's entry points refuse on the host, before anything reaches a device (no GPU needed: the pointers are
+never used)."""
+import ctypes as C
+
+import pytest
+
+ALIGNED = 1 << 20
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2509_00579_amd import binding, build
+    if not build.LIB.exists():
+        build.build()
+    binding.load()
+    return binding
+
+
+def _config(B, **kw):
+    d = dict(n_kv_heads=8, n_q_heads=32, head_dim=128, data_type=0, code_type=0, n_pages=100, n_tails=4, max_pages=16)
+    d.update(kw)
+    return B.PagedConfig(**d)
+
+
+def _memory(B, **kw):
+    d = dict.fromkeys(("d_k_codes", "d_v_codes", "d_scales", "d_k_tail", "d_v_tail", "d_fault"), ALIGNED)
+    d.update(kw)
+    return B.PagedTensors(**d)
+
+
+def _batch(B, **kw):
+    d = dict(batch=3, d_lens=ALIGNED, d_table=ALIGNED, d_tails=ALIGNED)
+    d.update(kw)
+    return B.PagedBatch(**d)
+
+
+def _new(B, **kw):
+    d = dict(n_tokens=10, d_starts=ALIGNED, d_k=ALIGNED, d_v=ALIGNED, k_stride=1024, v_stride=1024, d_q=0, d_q_out=0, q_stride=0,
+             q_out_stride=0, d_cos_sin=0, n_positions=0, rot_dim=0, interleaved=0, n_axes=1, sections=(C.c_int32 * 3)(), d_positions=0)
+    d.update(kw)
+    d["sections"] = (C.c_int32 * 3)(*d["sections"])
+    return B.PagedNew(**d)
+
+
+BAD_CONFIGS = [dict(n_kv_heads=0), dict(n_q_heads=33), dict(n_q_heads=0), dict(n_kv_heads=1, n_q_heads=33), dict(head_dim=96),
+               dict(data_type=2), dict(data_type=-1), dict(code_type=2), dict(n_pages=0), dict(n_tails=0), dict(max_pages=0),
+               dict(max_pages=(1 << 20) + 1)]
+BAD_MEMORY = [dict(d_k_codes=0), dict(d_v_codes=0), dict(d_scales=0), dict(d_k_tail=0), dict(d_v_tail=0), dict(d_fault=0),
+              dict(d_k_codes=ALIGNED + 8), dict(d_v_codes=ALIGNED + 4), dict(d_k_tail=ALIGNED + 2), dict(d_scales=ALIGNED + 4),
+              dict(d_fault=ALIGNED + 1)]
+BAD_BATCHES = [dict(batch=-1), dict(d_lens=0), dict(d_table=0), dict(d_tails=0), dict(batch=1 << 20)]
+
+
+def _refused(B, status):
+    assert status == B.ERR_INVALID_ARG
+    assert B.load().kvcomp_last_error()
+
+
+@pytest.mark.parametrize("i", range(len(BAD_CONFIGS) + len(BAD_MEMORY) + len(BAD_BATCHES)))
+def test_append_refuses_bad_caches(B, i):
+    bad = (BAD_CONFIGS + BAD_MEMORY + BAD_BATCHES)[i]
+    cfg, mem, seqs = _config(B), _memory(B), _batch(B)
+    if i < len(BAD_CONFIGS):
+        cfg = _config(B, **bad)
+    elif i < len(BAD_CONFIGS) + len(BAD_MEMORY):
+        mem = _memory(B, **bad)
+    else:
+        seqs = _batch(B, **bad)
+    _refused(B, B.load().kvcomp_paged_append(cfg, mem, seqs, _new(B), None))
+
+
+ROPE = dict(d_cos_sin=ALIGNED, n_positions=100, rot_dim=64, sections=(32,))
+Q = dict(d_q=ALIGNED, d_q_out=ALIGNED, q_stride=4096, q_out_stride=4096)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(n_tokens=-1), dict(d_starts=0), dict(n_tokens=1 << 26), dict(d_k=0), dict(d_v=0), dict(d_k=ALIGNED + 8), dict(d_v=ALIGNED + 2),
+    dict(k_stride=1023), dict(k_stride=1016), dict(v_stride=1028), dict(Q, d_q=0), dict(Q, d_q_out=0), dict(Q, q_stride=4088),
+    dict(Q, q_stride=4100), dict(Q, d_q=ALIGNED + 8), dict(Q, q_out_stride=8192), dict(ROPE, rot_dim=24), dict(ROPE, rot_dim=8),
+    dict(ROPE, rot_dim=144, sections=(72,)), dict(ROPE, n_positions=0), dict(ROPE, d_cos_sin=ALIGNED + 4), dict(ROPE, sections=(28,)),
+    dict(ROPE, n_axes=0), dict(ROPE, n_axes=4), dict(ROPE, n_axes=2, sections=(16, 16)),
+    dict(ROPE, n_axes=2, sections=(14, 18), d_positions=ALIGNED), dict(ROPE, n_axes=3, sections=(36, -8, 4), d_positions=ALIGNED)])
+def test_append_refuses_bad_tokens(B, bad):
+    _refused(B, B.load().kvcomp_paged_append(_config(B), _memory(B), _batch(B), _new(B, **bad), None))
+
+
+def test_nothing_to_append_is_fine(B):
+    lib = B.load()
+    assert lib.kvcomp_paged_append(_config(B), _memory(B), _batch(B), _new(B, n_tokens=0, d_k=0, d_v=0), None) == B.OK
+    assert lib.kvcomp_paged_append(_config(B), _memory(B), _batch(B, batch=0, d_lens=0), _new(B, n_tokens=0, d_starts=0), None) == B.OK
+
+
+def test_null_structures(B):
+    lib = B.load()
+    good = [_config(B), _memory(B), _batch(B), _new(B)]
+    for i in range(4):
+        args = list(good)
+        args[i] = None
+        _refused(B, lib.kvcomp_paged_append(*args, None))
+    _refused(B, lib.kvcomp_paged_check(None, None))
+    _refused(B, lib.kvcomp_paged_check(_memory(B, d_fault=0), None))
