@@ -323,6 +323,23 @@ typedef struct {        /* the new tokens of one append                         
 kvcomp_status kvcomp_paged_append(const kvcomp_paged_config *cfg, const kvcomp_paged_cache *cache,
                                   const kvcomp_paged_batch *seqs, const kvcomp_paged_new *fresh, void *stream);
 
+/* Device bytes of the attention calls' scratch for `cfg` (0 if it is invalid).  The caller ZERO-FILLS IT ONCE before the first
+ * call (it holds tickets, which every launch leaves at zero again).  Two launches that overlap in time, captured ones
+ * included, must not share one. */
+size_t kvcomp_paged_workspace_bytes(const kvcomp_paged_config *cfg);
+
+/* Decode attention, q_len rows per sequence (1, or a few drafted tokens; q_len * n_q_heads / n_kv_heads <= 32): row i of
+ * sequence b is d_q row b * q_len + i, stands at position lens[b] - q_len + i and sees the keys at positions up to its own
+ * and, with window > 0, above its own minus window.  out = softmax(scale * q.K^T) . V over those, sums in binary32, one
+ * rounding to the 16-bit type; a row that sees nothing is zero.  d_q, d_out: DEVICE [batch * q_len][n_q_heads][head_dim],
+ * 16-byte aligned, strides in elements between rows, multiples of 8.  max_len: the longest length as far as the caller
+ * knows (0: max_pages * 64); it sizes the launch only.  batch <= 4096.
+ * Errors: INVALID_ARG, CAPACITY (workspace too small), HIP. */
+kvcomp_status kvcomp_paged_attn_decode(const kvcomp_paged_config *cfg, const kvcomp_paged_cache *cache,
+                                       const kvcomp_paged_batch *seqs, const void *d_q, size_t q_stride, int q_len, float scale,
+                                       int window, int max_len, void *d_out, size_t out_stride, void *d_workspace,
+                                       size_t workspace_bytes, void *stream);
+
 /* What kernels flagged since the last check, once, and in this order: a page, tail or position out of range, or lengths or
  * starts that do not fit (STATE: such a sequence's tokens were not stored, its output rows are NaN; a token at a position
  * outside the table counts as one that holds NaN), Inf or NaN in what was appended (NONFINITE).  SYNCHRONISES `stream` and clears the flags. */

@@ -91,6 +91,8 @@ SIGNATURES = {
     "kvcomp_baseline_fp16_attn": (_i, [_cfgp, _vp, _vp, _i, _vp, _f, _vp, _vp, C.c_size_t, _i, _vp]),
     "kvcomp_baseline_fp16_attn_noalloc": (_i, [_cfgp, _vp, _vp, _i, _vp, _f, _vp, _i, _vp]),
     "kvcomp_paged_append": (_i, [_pcfg, _pmem, _pseq, _pnew, _vp]),
+    "kvcomp_paged_workspace_bytes": (C.c_size_t, [_pcfg]),
+    "kvcomp_paged_attn_decode": (_i, [_pcfg, _pmem, _pseq, _vp, C.c_size_t, _i, _f, _i, _i, _vp, C.c_size_t, _vp, C.c_size_t, _vp]),
     "kvcomp_paged_check": (_i, [_pmem, _vp]),
     "kvcomp_last_error": (C.c_char_p, []),
 }
@@ -427,6 +429,7 @@ class PagedCache:
         self._types = (head_dim, {torch.float16: 0, torch.bfloat16: 1}[dtype], int(codes == "e4m3"), n_pages, n_tails)
         self._memory = PagedTensors(*(x.data_ptr() for x in (*storage, self.fault)))
         self._config = {}
+        self._workspace = None
 
     def _cfg(self, max_pages):
         cfg = self._config.get(max_pages)
@@ -488,6 +491,33 @@ class PagedCache:
         new = PagedNew(n, sp, kp, vp, ks, vs, qp, op, qs, os_, cp, n_pos, rot, inter, axes, sections, pp)
         _check(self.lib.kvcomp_paged_append(self._cfg(table.shape[1]), self._memory, seqs, new, stream))
         return q_out
+
+    def new_workspace(self):
+        """Scratch of the attention calls, for one of them at a time."""
+        return torch.zeros(self.lib.kvcomp_paged_workspace_bytes(self._cfg(1)), dtype=torch.uint8, device=self.device)
+
+    def _scratch(self, workspace):
+        if workspace is None:
+            if self._workspace is None:
+                self._workspace = self.new_workspace()
+            return self._workspace
+        assert workspace.device == self.device and workspace.dtype is torch.uint8 and workspace.is_contiguous()
+        return workspace
+
+    def attn_decode(self, q, scale, lens, table, tails, q_len=1, window=0, max_len=0, out=None, workspace=None):
+        """Attention of q [batch * q_len, n_q_heads, head_dim], the last q_len tokens of every sequence, over the cache;
+        window: keys that a token sees, itself included (0: all before it); max_len: the longest length, if known."""
+        stream = self._on_device()
+        seqs = self._batch(lens, table, tails)
+        n = lens.shape[0] * q_len
+        if out is None:
+            out = torch.empty((n, self.Hq, self.D), dtype=self.dtype, device=self.device)
+        qp, qs = self._rows(q, n, self.Hq, "q")
+        op, os_ = self._rows(out, n, self.Hq, "out")
+        ws = self._scratch(workspace)
+        _check(self.lib.kvcomp_paged_attn_decode(self._cfg(table.shape[1]), self._memory, seqs, qp, qs, q_len, float(scale), window,
+                                                 max_len, op, os_, ws.data_ptr(), ws.numel(), stream))
+        return out
 
     def check(self):
         """Raises what kernels flagged since the last check (pages out of range, Inf or NaN appended); synchronises."""

@@ -5,9 +5,11 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-namespace kvc {
+#include <atomic>
 
-constexpr int kPBT = 64;  // tokens of a block and page
+#include "paged_plan.h"
+
+namespace kvc {
 
 enum : int { kF16 = 0, kBF16 = 1 };
 enum : int { kI8 = 0, kE4M3 = 1 };
@@ -41,7 +43,40 @@ struct PagedNew {
     int edge[2];  // first pair of the second and of the third axis
 };
 
+// One attention call: queries and outputs [rows][Hq][D] with their strides in elements.
+struct PagedAttn {
+    const uint16_t *__restrict__ q;
+    uint16_t *__restrict__ out;
+    size_t q_stride, out_stride;
+    float scale;  // times log2(e): the softmax runs on powers of two
+    int window;   // keys that a row sees, 0 = all before it
+    uint32_t *tickets;
+    float *partials;
+};
+
+constexpr int kDecodeRows = 32;       // query rows per KV head that a decode call may have
+constexpr int kDecodeWGs = 256;       // its largest grid
+constexpr int kMaxDecodeBatch = 4096;
+// Workspace: tickets, then two partial states per workgroup (o[D], m, l of each row, padded to whole 16 bytes).
+constexpr int kTicketWords = 1024;
+constexpr int partial_pitch(int D) { return D + 4; }
+
+hipError_t launch_paged_decode(const PagedGeo &g, const PagedAttn &a, int q_len, int max_len, int head_dim, int data_type, int code_type,
+                               hipStream_t s);
 hipError_t launch_paged_append(const PagedGeo &g, const PagedNew &n, int head_dim, int data_type, int code_type, hipStream_t s);
+
+// Lets a kernel have `most` bytes of dynamic LDS on the current device; `done` remembers for which devices (a bit each) that has
+// been said.
+inline hipError_t allow_lds(const void *kernel, size_t most, std::atomic<uint64_t> &done) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (done.load(std::memory_order_acquire) & bit)) return hipSuccess;
+    e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+    if (e == hipSuccess && dev < 64) done.fetch_or(bit, std::memory_order_release);
+    return e;
+}
 
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half8v __attribute__((ext_vector_type(8)));
@@ -75,6 +110,61 @@ __device__ __forceinline__ uint32_t narrow2(float a, float b) {
         return __builtin_bit_cast(uint32_t, v);
     }
 }
+// Eight codes as eight fp16 values, exactly.  int8: the bytes with their sign bit turned become the low bits of 1024 + 128 + code.
+template <int C>
+__device__ __forceinline__ half8v widen8(uint32_t a, uint32_t b) {
+    half2v r[4];
+    if constexpr (C == kI8) {
+        a ^= 0x80808080u;
+        b ^= 0x80808080u;
+        const half2v off = {(_Float16)1152.f, (_Float16)1152.f};
+        r[0] = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, a, 0x04010400u)) - off;
+        r[1] = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, a, 0x04030402u)) - off;
+        r[2] = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u)) - off;
+        r[3] = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u)) - off;
+    } else {
+        r[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false);
+        r[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true);
+        r[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false);
+        r[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true);
+    }
+    return half8v{r[0][0], r[0][1], r[1][0], r[1][1], r[2][0], r[2][1], r[3][0], r[3][1]};
+}
+
+// bf16 values reach the fp16 matrix instructions times a power of two that brings the largest of them to 2^14..2^15: a value is
+// then exact unless it is below 2^-28 of that one, and off by at most 2^-40 of it otherwise.
+__device__ __forceinline__ int bf16_shift(uint32_t largest_bits) { return 141 - (int)(largest_bits >> 7); }
+__device__ __forceinline__ uint32_t bf16_to_half2(uint32_t w, int shift) {
+    const half2v v = {(_Float16)ldexpf(wide_lo<kBF16>(w), shift), (_Float16)ldexpf(wide_hi<kBF16>(w), shift)};
+    return __builtin_bit_cast(uint32_t, v);
+}
+// The largest finite magnitude among the two values of a word and `m` (a bit pattern).
+__device__ __forceinline__ uint32_t bf16_largest(uint32_t m, uint32_t w) {
+    const uint32_t lo = w & 0x7fffu, hi = (w >> 16) & 0x7fffu;
+    m = lo < 0x7f80u && lo > m ? lo : m;
+    return hi < 0x7f80u && hi > m ? hi : m;
+}
+
+// Across the four groups of 16 lanes of a wave, and across its halves.
+__device__ __forceinline__ float max_rows(float v) {
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float sum_rows(float v) {
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+__device__ __forceinline__ uint32_t max_rows_u(uint32_t v) {
+    auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = a[0] > a[1] ? a[0] : a[1];
+    a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return a[0] > a[1] ? a[0] : a[1];
+}
+
 template <int T>
 constexpr uint32_t kInfBits = T == kBF16 ? 0x7f80u : 0x7c00u;  // magnitudes from here on are Inf or NaN
 template <int T>

@@ -117,6 +117,52 @@ kvcomp_status kvcomp_paged_append(const kvcomp_paged_config *cfg, const kvcomp_p
     return KVCOMP_OK;
 }
 
+size_t kvcomp_paged_workspace_bytes(const kvcomp_paged_config *cfg) {
+    if (check_config(cfg)) return 0;
+    return 4 * (kTicketWords + (size_t)2 * kDecodeWGs * kDecodeRows * partial_pitch(cfg->head_dim));
+}
+
+// what both attention calls are given; sets up `a`
+static kvcomp_status check_attn(const kvcomp_paged_config *cfg, const void *d_q, size_t q_stride, float scale, int window, void *d_out,
+                                size_t out_stride, void *d_workspace, size_t workspace_bytes, PagedAttn *a) {
+    kvcomp_status st;
+    if ((st = check_rows("d_q", d_q, q_stride, cfg->n_q_heads, cfg->head_dim))) return st;
+    if ((st = check_rows("d_out", d_out, out_stride, cfg->n_q_heads, cfg->head_dim))) return st;
+    if (!d_workspace || !aligned16(d_workspace)) return fail(KVCOMP_ERR_INVALID_ARG, "the workspace must be 16-byte aligned");
+    if (workspace_bytes < kvcomp_paged_workspace_bytes(cfg)) return fail(KVCOMP_ERR_CAPACITY, "workspace too small");
+    if (!(scale - scale == 0.f)) return fail(KVCOMP_ERR_INVALID_ARG, "scale must be finite");
+    if (window < 0) return fail(KVCOMP_ERR_INVALID_ARG, "window is negative");
+    a->q = static_cast<const uint16_t *>(d_q);
+    a->out = static_cast<uint16_t *>(d_out);
+    a->q_stride = q_stride;
+    a->out_stride = out_stride;
+    a->scale = scale * 1.44269504088896f;
+    a->window = window > kMaxPagesPerSeq * kPBT ? 0 : window;
+    a->tickets = static_cast<uint32_t *>(d_workspace);
+    a->partials = static_cast<float *>(d_workspace) + kTicketWords;
+    return KVCOMP_OK;
+}
+
+kvcomp_status kvcomp_paged_attn_decode(const kvcomp_paged_config *cfg, const kvcomp_paged_cache *cache,
+                                       const kvcomp_paged_batch *seqs, const void *d_q, size_t q_stride, int q_len, float scale,
+                                       int window, int max_len, void *d_out, size_t out_stride, void *d_workspace,
+                                       size_t workspace_bytes, void *stream) {
+    PagedGeo g;
+    PagedAttn a;
+    kvcomp_status st = check_all(cfg, cache, seqs, &g);
+    if (st) return st;
+    if (q_len < 1 || q_len > kDecodeRows || q_len * g.G > kDecodeRows)
+        return fail(KVCOMP_ERR_INVALID_ARG, "q_len must be at least 1, and q_len times the group of query heads at most %d", kDecodeRows);
+    if (g.batch > kMaxDecodeBatch) return fail(KVCOMP_ERR_INVALID_ARG, "more than %d sequences", kMaxDecodeBatch);
+    if ((long long)g.batch * g.H * g.max_pages > 0x7fffffffll)
+        return fail(KVCOMP_ERR_INVALID_ARG, "more than 2^31 - 1 sequences times KV heads times max_pages");
+    if (max_len < 0) return fail(KVCOMP_ERR_INVALID_ARG, "max_len is negative");
+    if (!g.batch) return KVCOMP_OK;
+    if ((st = check_attn(cfg, d_q, q_stride, scale, window, d_out, out_stride, d_workspace, workspace_bytes, &a))) return st;
+    HIP_TRY(launch_paged_decode(g, a, q_len, max_len, cfg->head_dim, cfg->data_type, cfg->code_type, static_cast<hipStream_t>(stream)));
+    return KVCOMP_OK;
+}
+
 kvcomp_status kvcomp_paged_check(const kvcomp_paged_cache *cache, void *stream) {
     if (!cache || !cache->d_fault) return fail(KVCOMP_ERR_INVALID_ARG, "NULL argument");
     hipStream_t s = static_cast<hipStream_t>(stream);

@@ -1,0 +1,599 @@
+// Decode attention over the paged cache of 8-bit codes: up to 32 query rows per KV head (a token or a few drafted ones, times
+// the group of query heads).  out = sum_j p_j v_j / sum_j p_j with p_j = 2^(s_j - m), s_j = log2(e) scale q.k_j, one pass with
+// the running maximum m.
+//
+// Bound by HBM: every code is read once.  A tile is one block (64 tokens) of a KV head; the tiles of all sequences and heads
+// form one list that is dealt evenly to the waves, whatever the sequences' lengths are, so a wave has a range of tiles of
+// one head, or the end of one, some whole ones and the beginning of another.  States of heads that are spread over several
+// waves meet in LDS, over several workgroups in the workspace, where the last workgroup to arrive joins them in order.
+//
+// Both products run on the fp16 matrix cores, S^T = K Q^T and O^T = V^T P^T, with the codes as the left operand straight
+// from their 16-byte loads: K rows are tokens, V pages have channels as rows.  Row r of the s-th group of 16 tokens is token
+// 16 (r / 4) + 4 s + r % 4, so that lane group g receives the scores of tokens 16 g .. 16 g + 15: the very tokens whose V
+// codes its loads bring, and P needs no exchange between lanes.  Codes are exact in fp16.  P goes in as two fp16 parts (the matrix
+// cores have nothing else to do), 22 bits of it; the reference m is 15 below the largest score, so that fp16's smallest step,
+// 2^-24, is 2^-39 of the largest weight and thousands of faint keys keep theirs.  Scales multiply the products: K's the scores, V's the tile's sum.
+#include "huff_decode.cuh"
+#include "paged.cuh"
+#include "split_combine.cuh"
+
+namespace kvc {
+
+namespace {
+
+struct DecodeArgs {
+    PagedGeo g;
+    PagedAttn a;
+    int q_len, rows;
+};
+
+__device__ __forceinline__ float4v mfma16(half8v a, half8v b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ half8v as_half8(uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    return __builtin_bit_cast(half8v, make_uint4(x, y, z, w));
+}
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+constexpr float kRefBelow = 15.f;
+constexpr float kNan = __builtin_nanf("");
+
+// T, C: types; D: channels; R: groups of 16 query rows.
+template <int T, int C, int D, int R>
+struct Wave {
+    static constexpr int CT = D / 16;  // channels CT r + i, i < CT, are row r of the i-th product with V
+    static constexpr int KJ = D / 64, KS = D / 32;
+    const DecodeArgs &p;
+    const int lane, n, g4;
+    half8v qf[R][KS];
+    float q_factor[R];
+    int q_place[R];  // token of the row among the call's
+    float m[R], l[R];
+    float4v o[R][CT];
+    uint4 kr[4][KJ], vr[CT];
+
+    __device__ __forceinline__ Wave(const DecodeArgs &p_, int lane_) : p(p_), lane(lane_), n(lane_ & 15), g4(lane_ >> 4) {
+#pragma unroll
+        for (int r = 0; r < R; r++) q_place[r] = (16 * r + n) / p.g.G;
+    }
+
+    __device__ __forceinline__ void begin(int b, int h) {
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            const int row = 16 * r + n;
+            const bool have = row < p.rows;
+            const uint16_t *q = p.a.q + ((size_t)b * p.q_len + q_place[r]) * p.a.q_stride + (size_t)(h * p.g.G + row - q_place[r] * p.g.G) * D;
+            uint4 w[KS];
+#pragma unroll
+            for (int k = 0; k < KS; k++)
+                w[k] = have ? *reinterpret_cast<const uint4 *>(q + (k >> 1) * 64 + g4 * 16 + (k & 1) * 8) : make_uint4(0, 0, 0, 0);
+            q_factor[r] = 1.f;
+            if constexpr (T == kBF16) {
+                uint32_t big = 0;
+#pragma unroll
+                for (int k = 0; k < KS; k++) big = bf16_largest(bf16_largest(bf16_largest(bf16_largest(big, w[k].x), w[k].y), w[k].z), w[k].w);
+                big = max_rows_u(big);
+                const int shift = bf16_shift(big);
+                q_factor[r] = ldexpf(1.f, -shift);
+#pragma unroll
+                for (int k = 0; k < KS; k++)
+                    w[k] = make_uint4(bf16_to_half2(w[k].x, shift), bf16_to_half2(w[k].y, shift), bf16_to_half2(w[k].z, shift),
+                                      bf16_to_half2(w[k].w, shift));
+            }
+#pragma unroll
+            for (int k = 0; k < KS; k++) qf[r][k] = __builtin_bit_cast(half8v, w[k]);
+            m[r] = -INFINITY;
+            l[r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < CT; i++) o[r][i] = float4v{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+
+    __device__ __forceinline__ int token_of(int s) const { return 16 * (n >> 2) + 4 * s + (n & 3); }
+
+    __device__ __forceinline__ void load_k(int page, int h) {
+        const uint8_t *t = p.g.k_codes + ((size_t)page * p.g.H + h) * kPBT * D + 16 * g4;
+#pragma unroll
+        for (int s = 0; s < 4; s++)
+#pragma unroll
+            for (int j = 0; j < KJ; j++) kr[s][j] = *reinterpret_cast<const uint4 *>(t + token_of(s) * D + 64 * j);
+    }
+    __device__ __forceinline__ void load_v(int page, int h) {
+        const uint8_t *t = p.g.v_codes + ((size_t)page * p.g.H + h) * kPBT * D + 16 * g4;
+#pragma unroll
+        for (int i = 0; i < CT; i++) vr[i] = *reinterpret_cast<const uint4 *>(t + (CT * n + i) * kPBT);
+    }
+
+    // Scores of tokens base + 16 g4 + j, j < 16, in powers of two; hidden ones are -Inf whatever they were.
+    __device__ __forceinline__ void scores(const float4v (&s)[R][4], float factor, int base, int len, float (&x)[R][16]) const {
+        const int first_row = len - p.q_len;  // position of the call's first token
+        const bool masked = base + kPBT - 1 > first_row || (p.a.window > 0 && base + p.a.window < len);
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            const float f = factor * q_factor[r];
+#pragma unroll
+            for (int j = 0; j < 16; j++) x[r][j] = s[r][j >> 2][j & 3] * f;
+            if (masked) {
+                const int pos = first_row + q_place[r];
+                const int low = p.a.window > 0 ? pos - p.a.window : -1;
+#pragma unroll
+                for (int j = 0; j < 16; j++) {
+                    const int t = base + 16 * g4 + j;
+                    if (t > pos || t <= low) x[r][j] = -INFINITY;
+                }
+            }
+        }
+    }
+
+    // x becomes P as fp16 parts; returns what the state so far is to be multiplied with.
+    __device__ __forceinline__ void softmax(float (&x)[R][16], half8v (&hi)[R][2], half8v (&lo)[R][2], float (&alpha)[R]) {
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            float mx = x[r][0];
+#pragma unroll
+            for (int j = 1; j < 16; j++) mx = fmaxf(mx, x[r][j]);
+            mx = fmaxf(fmaxf(m[r], max_rows(mx) - kRefBelow), kLowestRef);
+            alpha[r] = __builtin_amdgcn_exp2f(m[r] - mx);
+            m[r] = mx;
+            float sum = 0.f;
+            uint32_t ph[8], pl[8];
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+                const float a = __builtin_amdgcn_exp2f(x[r][j] - mx), b = __builtin_amdgcn_exp2f(x[r][j + 1] - mx);
+                sum += a + b;
+                const auto h = __builtin_amdgcn_cvt_pkrtz(a, b);
+                ph[j >> 1] = __builtin_bit_cast(uint32_t, h);
+                pl[j >> 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a - (float)h[0], b - (float)h[1]));
+            }
+            l[r] = l[r] * alpha[r] + sum;
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                hi[r][k] = as_half8(ph[4 * k], ph[4 * k + 1], ph[4 * k + 2], ph[4 * k + 3]);
+                lo[r][k] = as_half8(pl[4 * k], pl[4 * k + 1], pl[4 * k + 2], pl[4 * k + 3]);
+            }
+        }
+    }
+
+    __device__ __forceinline__ void add_v(int i, half8v v0, half8v v1, const half8v (&hi)[R][2], const half8v (&lo)[R][2],
+                                          const float (&alpha)[R], float factor) {
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            float4v acc = {0.f, 0.f, 0.f, 0.f};
+            acc = mfma16(v0, hi[r][0], acc);
+            acc = mfma16(v1, hi[r][1], acc);
+            acc = mfma16(v0, lo[r][0], acc);
+            acc = mfma16(v1, lo[r][1], acc);
+#pragma unroll
+            for (int k = 0; k < 4; k++) o[r][i][k] = fmaf(acc[k], factor, o[r][i][k] * alpha[r]);
+        }
+    }
+
+    // Tiles [i0, i1) of a head whose first tile is `first`.
+    __device__ __forceinline__ void run(int b, int h, int first, int i0, int i1, int len) {
+        const int whole = min(i1, len / kPBT - first);  // those that are pages
+        const int32_t *pages = p.g.table + (size_t)b * p.g.max_pages + first;
+        if (i0 < whole) {
+            int page, next = 0;
+            float ks, vs, ks_next = 0.f, vs_next = 0.f;
+            auto scales = [&](int &pg, float &k, float &v) {
+                const bool ok = (unsigned)pg < (unsigned)p.g.n_pages;
+                if (!ok) {
+                    if (lane == 0) flag(p.g.fault, kFaultPage);
+                    pg = 0;
+                }
+                const float *sc = p.g.scales + ((size_t)pg * p.g.H + h) * 2;
+                k = ok ? sc[0] : kNan;
+                v = sc[1];
+            };
+            page = uniform(pages[i0]);
+            if (i0 + 1 < whole) next = uniform(pages[i0 + 1]);
+            scales(page, ks, vs);
+            load_k(page, h);
+            load_v(page, h);
+            for (int i = i0; i < whole; i++) {
+                float4v s[R][4];
+#pragma unroll
+                for (int t = 0; t < 4; t++) {
+#pragma unroll
+                    for (int r = 0; r < R; r++) s[r][t] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int j = 0; j < KJ; j++) {
+                        const half8v k0 = widen8<C>(kr[t][j].x, kr[t][j].y), k1 = widen8<C>(kr[t][j].z, kr[t][j].w);
+#pragma unroll
+                        for (int r = 0; r < R; r++) {
+                            s[r][t] = mfma16(k0, qf[r][2 * j], s[r][t]);
+                            s[r][t] = mfma16(k1, qf[r][2 * j + 1], s[r][t]);
+                        }
+                    }
+                }
+                const bool more = i + 1 < whole;
+                if (more) {
+                    scales(next, ks_next, vs_next);
+                    load_k(next, h);
+                }
+                float x[R][16], alpha[R];
+                half8v hi[R][2], lo[R][2];
+                scores(s, ks * p.a.scale, (first + i) * kPBT, len, x);
+                softmax(x, hi, lo, alpha);
+#pragma unroll
+                for (int c = 0; c < CT; c++)
+                    add_v(c, widen8<C>(vr[c].x, vr[c].y), widen8<C>(vr[c].z, vr[c].w), hi, lo, alpha, vs);
+                if (more) {
+                    load_v(next, h);
+                    ks = ks_next;
+                    vs = vs_next;
+                    if (i + 2 < whole) next = uniform(pages[i + 2]);
+                }
+            }
+        }
+        if (whole < i1) unfinished(b, h, len);
+    }
+
+    // The block that is still in 16 bits: K as it is, V turned in registers, rows behind the end left out.
+    __device__ __forceinline__ void unfinished(int b, int h, int len) {
+        const int count = len % kPBT;
+        const size_t at = ((size_t)uniform(p.g.tails[b]) * p.g.H + h) * kPBT * D;
+        uint4 kt[4][KS];
+        uint32_t vt[16][CT / 2];  // token 16 g4 + j, channels CT n ..
+#pragma unroll
+        for (int s = 0; s < 4; s++) {
+            const uint16_t *k = p.g.k_tail + at + min(token_of(s), count - 1) * D + 16 * g4;
+#pragma unroll
+            for (int x = 0; x < KS; x++) kt[s][x] = *reinterpret_cast<const uint4 *>(k + (x >> 1) * 64 + (x & 1) * 8);
+        }
+#pragma unroll
+        for (int j = 0; j < 16; j++) {
+            const uint16_t *v = p.g.v_tail + at + min(16 * g4 + j, count - 1) * D + CT * n;
+            if constexpr (CT == 8) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(v);
+                vt[j][0] = w.x; vt[j][1] = w.y; vt[j][2] = w.z; vt[j][3] = w.w;
+            } else {
+                const uint2 w = *reinterpret_cast<const uint2 *>(v);
+                vt[j][0] = w.x; vt[j][1] = w.y;
+            }
+        }
+        float k_factor = 1.f, v_factor = 1.f;
+        if constexpr (T == kBF16) {
+            uint32_t mk = 0, mv = 0;
+#pragma unroll
+            for (int s = 0; s < 4; s++)
+#pragma unroll
+                for (int x = 0; x < KS; x++)
+                    mk = bf16_largest(bf16_largest(bf16_largest(bf16_largest(mk, kt[s][x].x), kt[s][x].y), kt[s][x].z), kt[s][x].w);
+#pragma unroll
+            for (int j = 0; j < 16; j++)
+#pragma unroll
+                for (int w = 0; w < CT / 2; w++) mv = bf16_largest(mv, vt[j][w]);
+            mk = max_rows_u(mk);
+            mv = max_rows_u(mv);
+            mk = max(mk, dpp_u<kDppXor1>(mk)); mv = max(mv, dpp_u<kDppXor1>(mv));
+            mk = max(mk, dpp_u<kDppXor2>(mk)); mv = max(mv, dpp_u<kDppXor2>(mv));
+            mk = max(mk, dpp_u<kDppHalfMirror>(mk)); mv = max(mv, dpp_u<kDppHalfMirror>(mv));
+            mk = max(mk, dpp_u<kDppMirror>(mk)); mv = max(mv, dpp_u<kDppMirror>(mv));
+            const int sk = bf16_shift(mk), sv = bf16_shift(mv);
+            k_factor = ldexpf(1.f, -sk);
+            v_factor = ldexpf(1.f, -sv);
+#pragma unroll
+            for (int s = 0; s < 4; s++)
+#pragma unroll
+                for (int x = 0; x < KS; x++)
+                    kt[s][x] = make_uint4(bf16_to_half2(kt[s][x].x, sk), bf16_to_half2(kt[s][x].y, sk), bf16_to_half2(kt[s][x].z, sk),
+                                          bf16_to_half2(kt[s][x].w, sk));
+#pragma unroll
+            for (int j = 0; j < 16; j++)
+#pragma unroll
+                for (int w = 0; w < CT / 2; w++) vt[j][w] = bf16_to_half2(vt[j][w], sv);
+        }
+        float4v s[R][4];
+#pragma unroll
+        for (int t = 0; t < 4; t++)
+#pragma unroll
+            for (int r = 0; r < R; r++) {
+                s[r][t] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int x = 0; x < KS; x++) s[r][t] = mfma16(__builtin_bit_cast(half8v, kt[t][x]), qf[r][x], s[r][t]);
+            }
+        float x[R][16], alpha[R];
+        half8v hi[R][2], lo[R][2];
+        scores(s, k_factor * p.a.scale, len - count, len, x);
+        softmax(x, hi, lo, alpha);
+#pragma unroll
+        for (int j = 0; j < 16; j++)
+#pragma unroll
+            for (int w = 0; w < CT / 2; w++) vt[j][w] = 16 * g4 + j < count ? vt[j][w] : 0u;
+#pragma unroll
+        for (int c = 0; c < CT; c++) {
+            uint32_t a[8];  // tokens 2 k and 2 k + 1 of channel CT n + c
+#pragma unroll
+            for (int k = 0; k < 8; k++)
+                a[k] = __builtin_amdgcn_perm(vt[2 * k + 1][c >> 1], vt[2 * k][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
+            add_v(c, as_half8(a[0], a[1], a[2], a[3]), as_half8(a[4], a[5], a[6], a[7]), hi, lo, alpha, v_factor);
+        }
+    }
+
+    // Lane (n, g4) holds channels CT (4 g4 + k) + c of row 16 r + n.
+    __device__ __forceinline__ void store(int b, int h) {
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            const float sum = sum_rows(l[r]), f = sum == 0.f ? 0.f : 1.f / sum;
+            const int row = 16 * r + n;
+            if (row >= p.rows) continue;
+            uint16_t *out = p.a.out + ((size_t)b * p.q_len + q_place[r]) * p.a.out_stride + (size_t)(h * p.g.G + row - q_place[r] * p.g.G) * D;
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                uint32_t w[CT / 2];
+#pragma unroll
+                for (int c = 0; c < CT; c += 2) w[c >> 1] = narrow2<T>(o[r][c][k] * f, o[r][c + 1][k] * f);
+                uint32_t *at = reinterpret_cast<uint32_t *>(out + CT * (4 * g4 + k));
+                if constexpr (CT == 8) *reinterpret_cast<uint4 *>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+                else *reinterpret_cast<uint2 *>(at) = make_uint2(w[0], w[1]);
+            }
+        }
+    }
+    __device__ __forceinline__ void park(float *slot) {
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            const float sum = sum_rows(l[r]);
+            const int row = 16 * r + n;
+            if (row >= p.rows) continue;
+            float *at = slot + row * partial_pitch(D);
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+#pragma unroll
+                for (int c = 0; c < CT; c += 4)
+                    *reinterpret_cast<float4 *>(at + CT * (4 * g4 + k) + c) =
+                        make_float4(o[r][c][k], o[r][c + 1][k], o[r][c + 2][k], o[r][c + 3][k]);
+            if (g4 == 0) {
+                at[D] = m[r];
+                at[D + 1] = sum;
+            }
+        }
+    }
+};
+
+constexpr size_t kDecodeLdsBytes = 159 * 1024;  // what the kernels may have apart from their own few words
+// Waves of a workgroup: the parked states of two segments per wave have to fit the LDS.
+constexpr int decode_waves(int R) { return R == 1 ? 8 : 4; }
+
+template <int T, int D>
+__device__ __forceinline__ void store_row4(const DecodeArgs &p, int b, int h, int row, int c, const float (&o)[4], float sum) {
+    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    const int place = row / p.g.G;
+    uint16_t *out = p.a.out + ((size_t)b * p.q_len + place) * p.a.out_stride + (size_t)(h * p.g.G + row - place * p.g.G) * D + c;
+    *reinterpret_cast<uint2 *>(out) = make_uint2(narrow2<T>(o[0] * f, o[1] * f), narrow2<T>(o[2] * f, o[3] * f));
+}
+
+template <int T, int C, int D, int R>
+__global__ __launch_bounds__(64 * decode_waves(R)) void paged_decode_kernel(DecodeArgs p) {
+    constexpr int kWaves = decode_waves(R), kThreads = 64 * kWaves, kSlots = 2 * kWaves, kPitch = partial_pitch(D), kQuads = D / 4;
+    extern __shared__ __align__(16) float s_dyn[];
+    __shared__ int s_b[kSlots], s_h[kSlots];
+    __shared__ uint32_t s_total, s_last[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int slot_floats = p.rows * kPitch;
+    uint32_t *before = reinterpret_cast<uint32_t *>(s_dyn + max(kSlots * slot_floats, kThreads * 4 + 2 * kDecodeWGs * p.rows));  // tiles of one head of the sequences before
+
+    auto sane = [&](int b, int len) {
+        return (unsigned)len <= (unsigned)p.g.max_pages * kPBT && (len % kPBT == 0 || (unsigned)p.g.tails[b] < (unsigned)p.g.n_tails);
+    };
+    auto count_of = [&](int b) -> uint32_t {
+        const int len = p.g.lens[b];
+        return sane(b, len) && len > 0 ? (uint32_t)tiles_of(len, p.q_len, p.a.window).count : 0u;
+    };
+    if (wave == 0) {
+        uint32_t sum = 0;
+        for (int base = 0; base < p.g.batch; base += 64) {
+            const uint32_t mine = base + lane < p.g.batch ? count_of(base + lane) : 0u;
+            const uint32_t ex = wave_excl_scan(mine, lane);
+            if (base + lane < p.g.batch) before[base + lane] = sum + ex;
+            sum += __builtin_amdgcn_readlane(ex + mine, 63);
+        }
+        if (lane == 0) {
+            before[p.g.batch] = sum;
+            s_total = sum;
+        }
+    }
+    if (lane < 2) s_b[2 * wave + lane] = -1;
+    __syncthreads();
+    // empty places: zeros; those that do not fit: NaN
+    for (int b = blockIdx.x; b < p.g.batch; b += gridDim.x) {
+        if (before[b + 1] != before[b]) continue;
+        const int len = p.g.lens[b];
+        const bool ok = sane(b, len);
+        if (!ok && tid == 0) flag(p.g.fault, (unsigned)len <= (unsigned)p.g.max_pages * kPBT ? kFaultTail : kFaultLength);
+        const uint32_t w = ok ? 0u : kNanBits<T> * 0x10001u;
+        const int per_row = p.g.H * p.g.G * D / 8;
+        for (int i = tid; i < p.q_len * per_row; i += kThreads)
+            *reinterpret_cast<uint4 *>(p.a.out + ((size_t)b * p.q_len + i / per_row) * p.a.out_stride + (size_t)(i % per_row) * 8) = make_uint4(w, w, w, w);
+    }
+    const uint32_t H = p.g.H, total = s_total * H;
+    // no more workgroups than there are tiles for their waves
+    const uint32_t active = min((uint32_t)gridDim.x, (total + kWaves - 1) / kWaves), wg = blockIdx.x;
+    if (wg >= active) return;
+    const Deal deal(total, active);
+    const uint32_t wg_begin = deal.begin(wg), wg_end = deal.begin(wg + 1);
+    const Deal inner(wg_end - wg_begin, kWaves);
+    uint32_t t = uniform((int)(wg_begin + inner.begin(wave)));
+    const uint32_t t_end = uniform((int)(wg_begin + inner.begin(wave + 1)));
+
+    Wave<T, C, D, R> w(p, lane);
+    int b = 0, parked = 0;
+    if (t < t_end) {  // the sequence of the first tile
+        int lo = 0, hi = p.g.batch;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if ((uint32_t)uniform((int)before[mid]) * H <= t) lo = mid; else hi = mid;
+        }
+        b = lo;
+    }
+    while (t < t_end) {
+        uint32_t base = (uint32_t)uniform((int)before[b]), tiles = (uint32_t)uniform((int)before[b + 1]) - base;
+        if ((base + tiles) * H <= t) {
+            b++;
+            continue;
+        }
+        const uint32_t in_seq = t - base * H, h = in_seq / tiles, i0 = in_seq - h * tiles, i1 = min(tiles, i0 + (t_end - t));
+        const int len = uniform(p.g.lens[b]);
+        w.begin(b, (int)h);
+        w.run(b, (int)h, tiles_of(len, p.q_len, p.a.window).first, (int)i0, (int)i1, len);
+        if (i1 - i0 == tiles) {
+            w.store(b, (int)h);
+        } else {
+            w.park(s_dyn + (size_t)(2 * wave + parked) * slot_floats);
+            if (lane == 0) {
+                s_b[2 * wave + parked] = b;
+                s_h[2 * wave + parked] = (int)h;
+            }
+            parked++;
+        }
+        t += i1 - i0;
+    }
+    __syncthreads();
+
+    // Join the parked states of each head; a head that other workgroups have a part of leaves its state in the workspace.
+    int open = 0, open_b[2], open_h[2];
+    for (int s0 = 0; s0 < kSlots;) {
+        const int sb = uniform(s_b[s0]), sh = uniform(s_h[s0]);
+        if (sb < 0) {
+            s0++;
+            continue;
+        }
+        int s1 = s0 + 1;
+        while (s1 < kSlots && (uniform(s_b[s1]) < 0 || (uniform(s_b[s1]) == sb && uniform(s_h[s1]) == sh))) s1++;
+        const uint32_t base = before[sb], tiles = before[sb + 1] - base;
+        const uint32_t begin = uniform((int)(base * H + sh * tiles)), end = begin + uniform((int)tiles);
+        const bool complete = begin >= wg_begin && end <= wg_end;
+        for (int item = tid; item < p.rows * kQuads; item += kThreads) {
+            const int row = item / kQuads, c = (item - row * kQuads) * 4;
+            float top = -INFINITY;
+            for (int s = s0; s < s1; s++)
+                if (s_b[s] >= 0) top = fmaxf(top, s_dyn[s * slot_floats + row * kPitch + D]);
+            float sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int s = s0; s < s1; s++) {
+                if (s_b[s] < 0) continue;
+                const float *at = s_dyn + s * slot_floats + row * kPitch;
+                const float f = __builtin_amdgcn_exp2f(at[D] - top);
+                const float4 v = *reinterpret_cast<const float4 *>(at + c);
+                sum = fmaf(at[D + 1], f, sum);
+                acc[0] = fmaf(v.x, f, acc[0]);
+                acc[1] = fmaf(v.y, f, acc[1]);
+                acc[2] = fmaf(v.z, f, acc[2]);
+                acc[3] = fmaf(v.w, f, acc[3]);
+            }
+            if (complete) {
+                store_row4<T, D>(p, sb, sh, row, c, acc, sum);
+            } else {
+                float *at = p.a.partials + ((size_t)(2 * wg + (begin < wg_begin ? 0 : 1)) * p.rows + row) * kPitch;
+#pragma unroll
+                for (int k = 0; k < 4; k++) store_agent(at + c + k, acc[k]);
+                if (c == 0) {
+                    store_agent(at + D, top);
+                    store_agent(at + D + 1, sum);
+                }
+            }
+        }
+        if (!complete) {
+            open_b[open & 1] = sb;
+            open_h[open & 1] = sh;
+            open++;
+        }
+        s0 = s1;
+    }
+    if (!open) return;
+    // every wave: its partial stores have completed before the barrier is passed
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    for (int k = 0; k < open; k++) {
+        const uint32_t base = before[open_b[k]], tiles = before[open_b[k] + 1] - base, begin = base * H + open_h[k] * tiles;
+        const uint32_t from = deal.owner(begin), parts = deal.owner(begin + tiles - 1) - from + 1;
+        if (tid == 0) {
+            const uint32_t ticket = __hip_atomic_fetch_add(p.a.tickets + from, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            s_last[k] = ticket == parts - 1;
+        }
+        __syncthreads();
+        if (!s_last[k]) continue;
+        // the last to arrive: all parts' maxima and sums to LDS, then groups of threads take parts in turn
+        float *s_m = s_dyn + kThreads * 4, *s_l = s_m + (size_t)kDecodeWGs * p.rows;
+        auto part_at = [&](uint32_t i) { return p.a.partials + ((size_t)(2 * (from + i) + (i == 0 ? 1 : 0)) * p.rows) * kPitch; };
+        for (uint32_t i = tid; i < parts * p.rows; i += kThreads) {
+            const uint32_t part = i / p.rows, row = i - part * p.rows;
+            s_m[i] = load_agent(part_at(part) + row * kPitch + D);
+            s_l[i] = load_agent(part_at(part) + row * kPitch + D + 1);
+        }
+        __syncthreads();
+        const int items = p.rows * kQuads, groups = max(1, min(kThreads / items, (int)parts));
+        for (int at = 0; at < items; at += kThreads) {
+            const int local = groups > 1 ? tid % items : tid, group = groups > 1 ? tid / items : 0, item = at + local;
+            const bool live = item < items && group < groups;
+            float sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+            const int row = live ? item / kQuads : 0, c = live ? (item - row * kQuads) * 4 : 0;
+            if (live) {
+                float top = -INFINITY;
+                for (uint32_t i = 0; i < parts; i++) top = fmaxf(top, s_m[i * p.rows + row]);
+                for (uint32_t i = group; i < parts; i += groups) {
+                    const float f = __builtin_amdgcn_exp2f(s_m[i * p.rows + row] - top);
+                    const float *v = part_at(i) + row * kPitch + c;
+                    sum = fmaf(s_l[i * p.rows + row], f, sum);
+#pragma unroll
+                    for (int x = 0; x < 4; x++) acc[x] = fmaf(load_agent(v + x), f, acc[x]);
+                }
+            }
+            if (groups > 1) {  // one round then: items < threads
+                *reinterpret_cast<float4 *>(s_dyn + 4 * tid) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+                __syncthreads();
+                if (live && group == 0) {
+                    for (int gr = 1; gr < groups; gr++) {
+                        const float4 v = *reinterpret_cast<const float4 *>(s_dyn + 4 * (gr * items + local));
+                        acc[0] += v.x; acc[1] += v.y; acc[2] += v.z; acc[3] += v.w;
+                    }
+                    float top = -INFINITY;
+                    for (uint32_t i = 0; i < parts; i++) top = fmaxf(top, s_m[i * p.rows + row]);
+                    sum = 0.f;
+                    for (uint32_t i = 0; i < parts; i++) sum = fmaf(s_l[i * p.rows + row], __builtin_amdgcn_exp2f(s_m[i * p.rows + row] - top), sum);
+                }
+            }
+            if (live && group == 0) store_row4<T, D>(p, open_b[k], open_h[k], row, c, acc, sum);
+        }
+        if (tid == 0) __hip_atomic_store(p.a.tickets + from, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+    }
+}
+
+template <int T, int C, int D, int R>
+hipError_t launch(const DecodeArgs &p, int max_len, hipStream_t s) {
+    constexpr int kThreads = 64 * decode_waves(R);
+    const size_t states = (size_t)2 * decode_waves(R) * p.rows * partial_pitch(D), join = (size_t)kThreads * 4 + 2 * (size_t)kDecodeWGs * p.rows;
+    const size_t lds = 4 * ((states > join ? states : join) + p.g.batch + 1);
+    auto kernel = paged_decode_kernel<T, C, D, R>;
+    static std::atomic<uint64_t> allowed{0};
+    hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), kDecodeLdsBytes, allowed);
+    if (e != hipSuccess) return e;
+    if (lds > kDecodeLdsBytes) return hipErrorInvalidValue;
+    // tiles there could be: no more workgroups than they can give each wave one
+    const int pages = max_len > 0 && max_len < p.g.max_pages * kPBT ? (max_len + kPBT - 1) / kPBT : p.g.max_pages;
+    const size_t most = (size_t)p.g.batch * p.g.H * pages, wgs = (most + decode_waves(R) - 1) / decode_waves(R);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(wgs < (size_t)kDecodeWGs ? wgs : (size_t)kDecodeWGs)), dim3(kThreads), lds, s, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_decode(const PagedGeo &g, const PagedAttn &a, int q_len, int max_len, int head_dim, int data_type, int code_type,
+                               hipStream_t s) {
+    DecodeArgs p = {g, a, q_len, q_len * g.G};
+    auto by_rows = [&](auto t, auto c, auto d) {
+        if (p.rows <= 16) return launch<decltype(t)::value, decltype(c)::value, decltype(d)::value, 1>(p, max_len, s);
+        return launch<decltype(t)::value, decltype(c)::value, decltype(d)::value, 2>(p, max_len, s);
+    };
+    auto by_dim = [&](auto t, auto c) {
+        if (head_dim == 64) return by_rows(t, c, std::integral_constant<int, 64>());
+        return by_rows(t, c, std::integral_constant<int, 128>());
+    };
+    auto by_code = [&](auto t) {
+        if (code_type == kI8) return by_dim(t, std::integral_constant<int, kI8>());
+        return by_dim(t, std::integral_constant<int, kE4M3>());
+    };
+    if (data_type == kF16) return by_code(std::integral_constant<int, kF16>());
+    return by_code(std::integral_constant<int, kBF16>());
+}
+
+}  // namespace kvc

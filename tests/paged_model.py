@@ -39,22 +39,27 @@ class Sequences:
         self.v[b].extend(v)
 
 
-def held(cache, page_row, tail, length):
-    """K and V [length, H, D] float64 that a cache's codes and tail stand for."""
-    out = []
-    for which in (0, 1):
-        codes = (cache.v_codes if which else cache.k_codes).cpu().float().double()
-        scales = cache.scales.cpu().double()
-        last = (cache.v_tail if which else cache.k_tail).cpu().double()
-        parts = []
-        for j in range(length // BT):
-            page = int(page_row[j])
-            tile = codes[page] * scales[page, :, which][:, None, None]
-            parts.append((tile.transpose(1, 2) if which else tile).transpose(0, 1))
-        if length % BT:
-            parts.append(last[int(tail)].transpose(0, 1)[:length % BT])
-        out.append(torch.cat(parts) if parts else torch.zeros((0, codes.shape[1], cache.D), dtype=F64))
-    return out
+class Snapshot:
+    """What a cache holds now, on the CPU."""
+
+    def __init__(self, cache):
+        self.codes = [x.cpu() for x in (cache.k_codes, cache.v_codes)]
+        self.tails = [x.cpu() for x in (cache.k_tail, cache.v_tail)]
+        self.scales, self.H, self.D = cache.scales.cpu().double(), cache.H, cache.D
+
+    def held(self, page_row, tail, length):
+        """K and V [length, H, D] float64 that the codes and the tail stand for."""
+        out = []
+        for which in (0, 1):
+            parts = []
+            for j in range(length // BT):
+                page = int(page_row[j])
+                tile = self.codes[which][page].float().double() * self.scales[page, :, which][:, None, None]
+                parts.append((tile.transpose(1, 2) if which else tile).transpose(0, 1))
+            if length % BT:
+                parts.append(self.tails[which][int(tail)].double().transpose(0, 1)[:length % BT])
+            out.append(torch.cat(parts) if parts else torch.zeros((0, self.H, self.D), dtype=F64))
+        return out
 
 
 def check_stored(cache, seqs, table, tails, lens):
@@ -67,8 +72,9 @@ def check_stored(cache, seqs, table, tails, lens):
     eps = torch.finfo(cache.dtype).eps / 2
     tiny = {torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134}[cache.dtype]
     int8 = cache.k_codes.dtype is torch.int8
+    now = Snapshot(cache)
     for b, length in enumerate(lens):
-        got = held(cache, table[b], tails[b], length)
+        got = now.held(table[b], tails[b], length)
         if not length:
             continue
         for which, name in ((0, "K"), (1, "V")):

@@ -308,3 +308,203 @@ def test_append_captured_and_replayed(gpu):
         want, size = M.rotate(q.double(), rope.cos_sin.cpu(), pos)
         assert bool(((out.cpu().double() - want).abs() <= 3 * 2.0 ** -24 * size + 2.0 ** -11 * want.abs() * 1.001 + 2.0 ** -25).all())
         w.check()
+
+
+def _close(got, ref, size, spread, dtype):
+    """Attention's outputs against 64 bits.  The output is rounded once: eps / 2 of its value (or half the type's smallest step).
+    A score is off by what 128 or fewer products summed in binary32 and two or three factors lose, (128 + 8) * 2^-24 of the sum of
+    their magnitudes `spread` (bf16 in fp16 parts adds 2^-40 of the largest); numerators and denominator change by that share, and by
+    2^-21 for the exponential and the two fp16 parts; sums over the keys in binary32 with a rescaling per tile lose 64 * 2^-24
+    more of the weighted magnitudes `size`."""
+    got = got.cpu().double()
+    eps = torch.finfo(dtype).eps / 2
+    share = 2 * 136 * 2.0 ** -24 * spread + 2 * 2.0 ** -21 + 2 * 64 * 2.0 ** -24
+    tol = eps * ref.abs() + share * size * (1 + eps) + (2.0 ** -25 if dtype is torch.float16 else 2.0 ** -134)
+    err = (got - ref).abs()
+    assert bool((err <= tol).all()), (float((err - tol).max()), float((err / tol).max()))
+
+
+def _reference(w, rows, window, scale, q):
+    """Model attention of the last rows[b] tokens of every sequence over what the cache holds; q rows one after the other."""
+    out, size, spread, at = [], [], [], 0
+    now = M.Snapshot(w.cache)
+    for b, n in enumerate(rows):
+        k, v = now.held(w.table[b], w.tails[b], w.lens[b])
+        pos = torch.arange(w.lens[b] - n, w.lens[b])
+        for got, x in zip((out, size, spread), M.attention(q[at:at + n].double(), k, v, scale, pos, window)):
+            got.append(x)
+        at += n
+    return torch.cat(out), torch.cat(size), torch.cat(spread)
+
+
+def _decode(w, q_len, window=0, scale=None, **kw):
+    q = w.rand(w.batch * q_len, w.Hq, w.D).to(w.dtype)
+    scale = 1 / math.sqrt(w.D) if scale is None else scale
+    got = w.cache.attn_decode(q.cuda(), scale, _i32(w.lens), w.d_table, w.d_tails, q_len=q_len, window=window, **kw)
+    torch.cuda.synchronize()
+    ref, size, spread = _reference(w, [q_len] * w.batch, window, scale, q)
+    _close(got, ref, size, spread, w.dtype)
+    return q, got
+
+
+@pytest.mark.parametrize("dtype,codes", TYPES, ids=IDS)
+@pytest.mark.parametrize("H,G,D,q_len", [(1, 1, 128, 1), (2, 8, 128, 1), (3, 3, 64, 1), (2, 4, 64, 5), (1, 7, 128, 4), (2, 16, 128, 1),
+                                         (1, 32, 64, 1), (1, 1, 128, 32), (2, 5, 128, 6)])
+def test_decode(gpu, dtype, codes, H, G, D, q_len):
+    """Lengths from nothing to several blocks, whole and unfinished ones, one row to 32."""
+    w = World(gpu, 9, H, G, D, dtype, codes, 12, seed=H * G + D)
+    counts = [1, 0, 63, 64, 65, 700, 128, 7, 256]
+    k, v, _ = w.tokens(sum(counts))
+    w.append(counts, k, v)
+    _decode(w, q_len)
+    _decode(w, q_len, max_len=700)
+    _decode(w, q_len, scale=-0.3)
+    w.cache.check()
+
+
+@pytest.mark.parametrize("window", [1, 2, 63, 64, 65, 100, 1000, 1 << 30])
+def test_decode_sliding_window(gpu, window):
+    for dtype, codes, D, q_len in ((torch.float16, "int8", 64, 1), (torch.bfloat16, "e4m3", 128, 3)):
+        w = World(gpu, 6, 2, 4, D, dtype, codes, 6, seed=window % 97)
+        counts = [1, 64, 65, 200, 383, 0]
+        k, v, _ = w.tokens(sum(counts))
+        w.append(counts, k, v)
+        _decode(w, q_len, window)
+
+
+@pytest.mark.parametrize("batch,H,G,longest", [(1, 1, 1, 8000), (1, 2, 8, 5000), (3, 8, 2, 3000), (70, 2, 1, 300), (300, 1, 1, 64), (2, 1, 32, 2500)])
+def test_decode_split_over_waves_and_workgroups(gpu, batch, H, G, longest):
+    """Few long sequences, whose tiles are spread over many workgroups, and many short ones; twice on the same workspace, the
+    same bits both times."""
+    w = World(gpu, batch, H, G, 64, torch.float16, "int8", longest // 64 + 1, seed=batch)
+    rng = random.Random(batch)
+    counts = [longest] + [rng.randrange(longest + 1) for _ in range(batch - 1)]
+    k, v, _ = w.tokens(sum(counts))
+    n = 0
+    w.append(counts, k, v)
+    q, a = _decode(w, 1)
+    b = w.cache.attn_decode(q.cuda(), 1 / 8, _i32(w.lens), w.d_table, w.d_tails)
+    assert torch.equal(a, b)
+    ws = w.cache.new_workspace()
+    c = w.cache.attn_decode(q.cuda(), 1 / 8, _i32(w.lens), w.d_table, w.d_tails, workspace=ws)
+    assert torch.equal(a, c) and not ws[:4096].any()
+
+
+def test_decode_strides_and_rows_behind_the_batch(gpu):
+    w = World(gpu, 3, 2, 2, 64, torch.bfloat16, "int8", 3, seed=2)
+    counts = [70, 64, 10]
+    k, v, _ = w.tokens(144)
+    w.append(counts, k, v)
+    q, want = _decode(w, 2)
+    wide = torch.full((8, 4 * 64 + 24), 5.0, dtype=torch.bfloat16, device="cuda:0")
+    qs = torch.zeros((6, 3 * 256), dtype=torch.bfloat16, device="cuda:0")
+    qs[:, 256:512] = q.cuda().flatten(1)
+    got = wide[:6, 8:264].unflatten(1, (4, 64))
+    w.cache.attn_decode(qs[:, 256:512].unflatten(1, (4, 64)), 1 / 8, _i32(w.lens), w.d_table, w.d_tails, q_len=2, out=got)
+    assert torch.equal(got, want)
+    assert (wide[6:] == 5).all() and (wide[:, :8] == 5).all() and (wide[:, 264:] == 5).all()
+
+
+@pytest.mark.parametrize("dtype,codes", TYPES, ids=IDS)
+def test_decode_large_and_small_values(gpu, dtype, codes):
+    """Scores far apart, a key that takes all the weight, values near the ends of the type's range, queries of zeros."""
+    w = World(gpu, 4, 1, 4, 128, dtype, codes, 3, seed=3)
+    k, v, _ = w.tokens(4 * 130)
+    top = 6e4 if dtype is torch.float16 else 1e30
+    k[130:260] = (k[130:260].double() * 30).clamp(-top, top).to(dtype)
+    v[130:260] = (v[130:260].double() * (1e4 if dtype is torch.float16 else 1e30)).to(dtype)
+    v[260:390] = (v[260:390].double() * (1e-5 if dtype is torch.float16 else 1e-30)).to(dtype)
+    k[390:], v[390:] = 0, 0
+    w.append([130] * 4, k, v)
+    _decode(w, 1)
+    _decode(w, 1, scale=0.0)
+    q = torch.zeros((4, 4, 128), dtype=dtype, device="cuda:0")
+    got = w.cache.attn_decode(q, 1.0, _i32(w.lens), w.d_table, w.d_tails)
+    ref, size, spread = _reference(w, [1] * 4, 0, 1.0, q.cpu())
+    _close(got, ref, size, spread, dtype)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype,codes", TYPES, ids=IDS)
+def test_decode_non_finite_tokens_reach_only_the_rows_that_see_them(gpu, dtype, codes, D):
+    """Inf and NaN in a block and in an unfinished one, hidden by the causal order, by the window or by nothing."""
+    w = World(gpu, 3, 2, 1, D, dtype, codes, 3, seed=4)
+    k, v, _ = w.tokens(150 + 100 + 70)
+    v[3, 1, 5] = math.inf              # sequence 0, block 0, head 1
+    k[150 + 98, 0, 7] = math.nan       # sequence 1, unfinished block, head 0: hidden from the rows before
+    v[250 + 69, 0, 1] = -math.inf      # sequence 2, its last token
+    w.append([150, 100, 70], k, v)
+    for window in (0, 50):
+        q = w.rand(3 * 3, 2, D).to(dtype)
+        got = w.cache.attn_decode(q.cuda(), 0.1, _i32(w.lens), w.d_table, w.d_tails, q_len=3, window=window).cpu()
+        nan = torch.isnan(got)
+        want = torch.zeros_like(nan)
+        want[0:3, 1] = window == 0
+        want[4:6, 0] = True   # tokens 98 and 99
+        want[8, 0] = True
+        assert torch.equal(nan, want), window
+
+
+def test_decode_places_out_of_range(gpu):
+    """A page, a tail or a length that does not fit: NaN for that sequence, the check says so, the others are right."""
+    w = World(gpu, 4, 2, 2, 64, torch.float16, "int8", 3, seed=7)
+    k, v, _ = w.tokens(4 * 100)
+    w.append([100] * 4, k, v)
+    q, want = _decode(w, 1)
+    for what in ("page", "page_low", "tail", "tail_low", "length", "length_low"):
+        lens, table, tails = list(w.lens), w.table.clone(), w.tails.clone()
+        if what.startswith("page"):
+            table[1, 0] = -1 if what == "page_low" else w.cache.n_pages
+        elif what.startswith("tail"):
+            tails[1] = -1 if what == "tail_low" else w.cache.n_tails
+        else:
+            lens[1] = -1 if what == "length_low" else 193
+        got = w.cache.attn_decode(q.cuda(), 1 / 8, _i32(lens), _i32(table), _i32(tails))
+        assert torch.isnan(got[1]).all() and torch.equal(got[[0, 2, 3]], want[[0, 2, 3]]), what
+        with pytest.raises(gpu.KvcompError) as e:
+            w.cache.check()
+        assert e.value.status == gpu.ERR_STATE
+        w.cache.check()
+    table = w.table.clone()
+    table[:, 2] = 1 << 30  # not needed: the second block is unfinished
+    table[:, 1] = -7
+    assert torch.equal(w.cache.attn_decode(q.cuda(), 1 / 8, _i32(w.lens), _i32(table), w.d_tails), want)
+    w.cache.check()
+
+
+def test_decode_shared_pages_other_streams_and_replays(gpu):
+    """A prefix whose pages two sequences share; two streams with a workspace each; a captured step replayed while eager calls
+    run between."""
+    w = World(gpu, 2, 4, 4, 128, torch.bfloat16, "e4m3", 40, seed=8)
+    k, v, _ = w.tokens(2000)
+    k2, v2, _ = w.tokens(30)
+    w.append([2000, 0], k, v)
+    shared = w.table.clone()
+    shared[1, :30] = shared[0, :30]
+    for b in range(1920):
+        w.seqs.add(1, [w.seqs.k[0][b]], [w.seqs.size[0][b]], [w.seqs.v[0][b]])
+    w.table, w.d_table, w.lens[1] = shared, _i32(shared), 1920
+    w.append([0, 30], k2, v2)
+    q, want = _decode(w, 1)
+    lens, dq, out = _i32(w.lens), q.cuda(), torch.empty_like(want)
+    side, ws = torch.cuda.Stream(), w.cache.new_workspace()
+    side.wait_stream(torch.cuda.current_stream())
+    outs = []
+    for _ in range(10):
+        outs.append(w.cache.attn_decode(dq, 1 / math.sqrt(128), lens, w.d_table, w.d_tails))
+        with torch.cuda.stream(side):
+            outs.append(w.cache.attn_decode(dq, 1 / math.sqrt(128), lens, w.d_table, w.d_tails, workspace=ws))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want) for x in outs)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        w.cache.attn_decode(dq, 1 / math.sqrt(128), lens, w.d_table, w.d_tails, out=out, workspace=ws)
+    for shorter in (0, 1, 500, 0):
+        lens.copy_(_i32([w.lens[0] // 64 * 64 - 64 * (shorter // 64) if shorter else w.lens[0], w.lens[1]]))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = w.cache.attn_decode(dq, 1 / math.sqrt(128), lens, w.d_table, w.d_tails)
+        assert torch.equal(out, eager)
+        if not shorter:
+            assert torch.equal(out, want)
