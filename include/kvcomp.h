@@ -252,7 +252,7 @@ kvcomp_status kvcomp_probe_read_stream(const void *d_buf, size_t bytes, void *d_
  * of any lengths in pages of 64 tokens, rotates keys (and queries) on the way in, and is read by single tokens, drafted
  * tokens and whole prompt chunks.  The calls keep no state in the library: cache, lengths and page tables are the
  * caller's device memory, and lengths are read on the device, so that a captured step replays with the lengths of the day.
- * All calls are stream-ordered, launch one kernel each, allocate nothing and never synchronise, except kvcomp_paged_check.
+ * All calls are stream-ordered, launch a kernel or two, allocate nothing and never synchronise, except kvcomp_paged_check.
  * The current device must be the one that the memory is on.
  *
  * A block is 64 consecutive tokens of a sequence (tokens 64 j .. 64 j + 63), its page holds it for all KV heads:
@@ -339,6 +339,17 @@ kvcomp_status kvcomp_paged_attn_decode(const kvcomp_paged_config *cfg, const kvc
                                        const kvcomp_paged_batch *seqs, const void *d_q, size_t q_stride, int q_len, float scale,
                                        int window, int max_len, void *d_out, size_t out_stride, void *d_workspace,
                                        size_t workspace_bytes, void *stream);
+
+/* Attention of chunks of new tokens: rows starts[b] .. starts[b+1]-1 of d_q (d_starts: DEVICE int32 [batch + 1]) are the last
+ * tokens of sequence b, row starts[b] + i stands at position lens[b] - (starts[b+1] - starts[b]) + i and sees what a decode
+ * row at that position sees.  d_q, d_out: DEVICE [n_tokens][n_q_heads][head_dim]; rows of d_out outside every sequence's
+ * range, and those of a sequence whose starts do not fit into n_tokens, are left as they were.  max_new, max_len: the most new
+ * tokens and the longest length as far as the caller knows (0: no idea); they shape the launch only.  One kernel, and a
+ * second one where few rows over long sequences make it split the keys.  Errors: INVALID_ARG, CAPACITY, HIP. */
+kvcomp_status kvcomp_paged_attn_prefill(const kvcomp_paged_config *cfg, const kvcomp_paged_cache *cache,
+                                        const kvcomp_paged_batch *seqs, const void *d_q, size_t q_stride, const void *d_starts,
+                                        int n_tokens, float scale, int window, int max_new, int max_len, void *d_out,
+                                        size_t out_stride, void *d_workspace, size_t workspace_bytes, void *stream);
 
 /* What kernels flagged since the last check, once, and in this order: a page, tail or position out of range, or lengths or
  * starts that do not fit (STATE: such a sequence's tokens were not stored, its output rows are NaN; a token at a position

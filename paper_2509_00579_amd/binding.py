@@ -93,6 +93,8 @@ SIGNATURES = {
     "kvcomp_paged_append": (_i, [_pcfg, _pmem, _pseq, _pnew, _vp]),
     "kvcomp_paged_workspace_bytes": (C.c_size_t, [_pcfg]),
     "kvcomp_paged_attn_decode": (_i, [_pcfg, _pmem, _pseq, _vp, C.c_size_t, _i, _f, _i, _i, _vp, C.c_size_t, _vp, C.c_size_t, _vp]),
+    "kvcomp_paged_attn_prefill": (_i, [_pcfg, _pmem, _pseq, _vp, C.c_size_t, _vp, _i, _f, _i, _i, _i, _vp, C.c_size_t, _vp,
+                                       C.c_size_t, _vp]),
     "kvcomp_paged_check": (_i, [_pmem, _vp]),
     "kvcomp_last_error": (C.c_char_p, []),
 }
@@ -517,6 +519,23 @@ class PagedCache:
         ws = self._scratch(workspace)
         _check(self.lib.kvcomp_paged_attn_decode(self._cfg(table.shape[1]), self._memory, seqs, qp, qs, q_len, float(scale), window,
                                                  max_len, op, os_, ws.data_ptr(), ws.numel(), stream))
+        return out
+
+    def attn_prefill(self, q, scale, starts, lens, table, tails, max_new=0, max_len=0, window=0, out=None, workspace=None):
+        """Attention of chunks: rows starts[b] .. starts[b + 1] of q [n, n_q_heads, head_dim] are the last tokens of sequence b
+        (starts: int32 [batch + 1]); max_new, max_len: the longest chunk and length, if known."""
+        stream = self._on_device()
+        seqs = self._batch(lens, table, tails)
+        assert starts.dtype is torch.int32 and starts.device == self.device and starts.is_contiguous()
+        assert starts.shape == (lens.shape[0] + 1,), "starts: one entry per sequence and the end"
+        n = q.shape[0]
+        if out is None:
+            out = torch.empty((n, self.Hq, self.D), dtype=self.dtype, device=self.device)
+        qp, qs = self._rows(q, n, self.Hq, "q")
+        op, os_ = self._rows(out, n, self.Hq, "out")
+        ws = self._scratch(workspace)
+        _check(self.lib.kvcomp_paged_attn_prefill(self._cfg(table.shape[1]), self._memory, seqs, qp, qs, starts.data_ptr(), n,
+                                                  float(scale), window, max_new, max_len, op, os_, ws.data_ptr(), ws.numel(), stream))
         return out
 
     def check(self):

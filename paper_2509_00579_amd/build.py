@@ -11,7 +11,7 @@ CSRC = HERE / "csrc"
 LIB = HERE / "libkvcomp.so"
 OBJ = HERE / "_build"
 SOURCES = ["kvcomp_api.hip", "quantize.hip", "encode.hip", "attn_fused.hip", "attn_fp16.hip", "decompress.hip",
-           "paged_api.hip", "paged_append.hip", "paged_decode.hip"]
+           "paged_api.hip", "paged_append.hip", "paged_decode.hip", "paged_prefill.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
     "-fhip-fp32-correctly-rounded-divide-sqrt",

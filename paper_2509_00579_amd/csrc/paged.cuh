@@ -61,6 +61,11 @@ constexpr int kMaxDecodeBatch = 4096;
 constexpr int kTicketWords = 1024;
 constexpr int partial_pitch(int D) { return D + 4; }
 
+constexpr int kPrefillSplitWGs = 512;  // most workgroups of a prefill launch that splits the keys
+constexpr int kPrefillRows = 128;      // query rows of one of them
+
+hipError_t launch_paged_prefill(const PagedGeo &g, const PagedAttn &a, const int32_t *starts, int n_tokens, int max_new, int max_len,
+                                int head_dim, int data_type, int code_type, hipStream_t s);
 hipError_t launch_paged_decode(const PagedGeo &g, const PagedAttn &a, int q_len, int max_len, int head_dim, int data_type, int code_type,
                                hipStream_t s);
 hipError_t launch_paged_append(const PagedGeo &g, const PagedNew &n, int head_dim, int data_type, int code_type, hipStream_t s);

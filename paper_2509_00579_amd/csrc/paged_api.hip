@@ -119,7 +119,8 @@ kvcomp_status kvcomp_paged_append(const kvcomp_paged_config *cfg, const kvcomp_p
 
 size_t kvcomp_paged_workspace_bytes(const kvcomp_paged_config *cfg) {
     if (check_config(cfg)) return 0;
-    return 4 * (kTicketWords + (size_t)2 * kDecodeWGs * kDecodeRows * partial_pitch(cfg->head_dim));
+    const size_t decode = (size_t)2 * kDecodeWGs * kDecodeRows, prefill = (size_t)kPrefillSplitWGs * kPrefillRows;  // rows of states
+    return 4 * (kTicketWords + (decode > prefill ? decode : prefill) * partial_pitch(cfg->head_dim));
 }
 
 // what both attention calls are given; sets up `a`
@@ -160,6 +161,24 @@ kvcomp_status kvcomp_paged_attn_decode(const kvcomp_paged_config *cfg, const kvc
     if (!g.batch) return KVCOMP_OK;
     if ((st = check_attn(cfg, d_q, q_stride, scale, window, d_out, out_stride, d_workspace, workspace_bytes, &a))) return st;
     HIP_TRY(launch_paged_decode(g, a, q_len, max_len, cfg->head_dim, cfg->data_type, cfg->code_type, static_cast<hipStream_t>(stream)));
+    return KVCOMP_OK;
+}
+
+kvcomp_status kvcomp_paged_attn_prefill(const kvcomp_paged_config *cfg, const kvcomp_paged_cache *cache,
+                                        const kvcomp_paged_batch *seqs, const void *d_q, size_t q_stride, const void *d_starts,
+                                        int n_tokens, float scale, int window, int max_new, int max_len, void *d_out,
+                                        size_t out_stride, void *d_workspace, size_t workspace_bytes, void *stream) {
+    PagedGeo g;
+    PagedAttn a;
+    kvcomp_status st = check_all(cfg, cache, seqs, &g);
+    if (st) return st;
+    if (!d_starts || (reinterpret_cast<uintptr_t>(d_starts) & 3u)) return fail(KVCOMP_ERR_INVALID_ARG, "d_starts is NULL or not aligned");
+    if (n_tokens < 0 || max_new < 0 || max_len < 0) return fail(KVCOMP_ERR_INVALID_ARG, "n_tokens, max_new or max_len is negative");
+    if ((long long)n_tokens * cfg->n_q_heads > (1ll << 30)) return fail(KVCOMP_ERR_INVALID_ARG, "more than 2^30 tokens times query heads");
+    if (!g.batch || !n_tokens) return KVCOMP_OK;
+    if ((st = check_attn(cfg, d_q, q_stride, scale, window, d_out, out_stride, d_workspace, workspace_bytes, &a))) return st;
+    HIP_TRY(launch_paged_prefill(g, a, static_cast<const int32_t *>(d_starts), n_tokens, max_new, max_len, cfg->head_dim,
+                                 cfg->data_type, cfg->code_type, static_cast<hipStream_t>(stream)));
     return KVCOMP_OK;
 }
 

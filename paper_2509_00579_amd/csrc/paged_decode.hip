@@ -34,6 +34,11 @@ __device__ __forceinline__ half8v as_half8(uint32_t x, uint32_t y, uint32_t z, u
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 constexpr float kRefBelow = 15.f;
+// bf16: the accumulators hold 2^-40 of the sums, so that neither the largest values overflow them (2^15 of a weight, 2^26 keys)
+// nor the largest weight's of anything that a page holds (2^-100 and more) drops below binary32's normal range; the factor
+// is a multiplication of its own, since with it the smallest scales would.
+template <int T>
+constexpr float kVUnit = T == kBF16 ? 9.094947017729282e-13f : 1.f;
 constexpr float kNan = __builtin_nanf("");
 
 // T, C: types; D: channels; R: groups of 16 query rows.
@@ -162,7 +167,7 @@ struct Wave {
             acc = mfma16(v0, lo[r][0], acc);
             acc = mfma16(v1, lo[r][1], acc);
 #pragma unroll
-            for (int k = 0; k < 4; k++) o[r][i][k] = fmaf(acc[k], factor, o[r][i][k] * alpha[r]);
+            for (int k = 0; k < 4; k++) o[r][i][k] = fmaf(T == kBF16 ? acc[k] * kVUnit<T> : acc[k], factor, o[r][i][k] * alpha[r]);
         }
     }
 
@@ -313,7 +318,7 @@ struct Wave {
     __device__ __forceinline__ void store(int b, int h) {
 #pragma unroll
         for (int r = 0; r < R; r++) {
-            const float sum = sum_rows(l[r]), f = sum == 0.f ? 0.f : 1.f / sum;
+            const float sum = sum_rows(l[r]), f = sum == 0.f ? 0.f : (1.f / kVUnit<T>) / sum;
             const int row = 16 * r + n;
             if (row >= p.rows) continue;
             uint16_t *out = p.a.out + ((size_t)b * p.q_len + q_place[r]) * p.a.out_stride + (size_t)(h * p.g.G + row - q_place[r] * p.g.G) * D;
@@ -355,7 +360,7 @@ constexpr int decode_waves(int R) { return R == 1 ? 8 : 4; }
 
 template <int T, int D>
 __device__ __forceinline__ void store_row4(const DecodeArgs &p, int b, int h, int row, int c, const float (&o)[4], float sum) {
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    const float f = sum == 0.f ? 0.f : (1.f / kVUnit<T>) / sum;
     const int place = row / p.g.G;
     uint16_t *out = p.a.out + ((size_t)b * p.q_len + place) * p.a.out_stride + (size_t)(h * p.g.G + row - place * p.g.G) * D + c;
     *reinterpret_cast<uint2 *>(out) = make_uint2(narrow2<T>(o[0] * f, o[1] * f), narrow2<T>(o[2] * f, o[3] * f));

@@ -1,0 +1,481 @@
+// Attention of prompt chunks over the paged cache of 8-bit codes: ragged chunks, causal, optionally within a sliding window.
+//
+// Bound by the matrix cores.  A workgroup owns one KV head and a tile of query rows: consecutive tokens times the group of query
+// heads, so that every K and V block it stages serves whole groups.  The codes of a block are widened to fp16 once per
+// workgroup, on their way to LDS (two buffers, one barrier a block); a wave multiplies its 32 rows, S^T = K Q^T and
+// O^T = V^T P^T on 32x32x16 products.  Row r of K's 32 is token 16 (r / 16) + 8 (r / 4 % 2) + 4 (r / 8 % 2) + r % 4, so that a
+// lane receives the scores of eight consecutive tokens: its part of P^T for the second product, without an exchange.
+//
+// K's scale multiplies the scores.  V's scale is 2^e times a mantissa: the mantissa is added to the exponents of P (and taken
+// out of their sum again), 2^e goes into the codes as they are widened, relative to the largest e so far: exact down to 2^-24
+// of it (int8) or 2^-15 (e4m3), off by 2^-25 of the largest scale below that.  So a tile's product adds to the output's
+// accumulators as it is.  P is rounded to fp16 (11 bits, relative to each weight: the reference leaves 2^8 to 2^14 above
+// one, so weights down to 2^-22 of a row's largest keep all of them), and the sum of the weights is taken from the rounded ones.
+// The reference moves only when a score would pass 2^14 above it, which spares most tiles the rescaling of the accumulators.
+//
+// Few rows over a long axis: the keys are split among workgroups, and a second launch joins their states.
+#include <algorithm>
+
+#include "huff_decode.cuh"
+#include "paged.cuh"
+#include "split_combine.cuh"
+
+namespace kvc {
+
+namespace {
+
+constexpr int kPreWaves = 4, kPreRows = 32 * kPreWaves, kPreThreads = 64 * kPreWaves;
+static_assert(kPreRows == kPrefillRows, "the workspace is laid out for them");
+constexpr float kRefLead = 8.f, kRefMost = 14.f;
+
+struct PrefillArgs {
+    PagedGeo g;
+    PagedAttn a;
+    int n_tokens, units, splits;
+    int per_tile;  // tokens of a row tile
+    const int32_t *__restrict__ starts;
+};
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ float16v mfma32(half8v a, half8v b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+// The row tile of a unit: which sequence, its first token among the sequence's new ones.
+struct RowTile {
+    int b, start, fresh, len, place;
+    bool bad;
+};
+// All lanes of a wave together.  b < 0: no such unit.
+__device__ __forceinline__ RowTile find_tile(const PrefillArgs &p, int unit, int lane) {
+    RowTile r;
+    r.b = -1;
+    r.bad = false;
+    for (int base = 0; base < p.g.batch && r.b < 0; base += 64) {
+        int tiles = 0;
+        if (base + lane < p.g.batch) {
+            const int s0 = p.starts[base + lane], s1 = p.starts[base + lane + 1];
+            if (s0 >= 0 && s1 > s0 && s1 <= p.n_tokens) tiles = (s1 - s0 + p.per_tile - 1) / p.per_tile;
+            else if (s1 != s0 || s0 < 0 || s1 > p.n_tokens) flag(p.g.fault, kFaultLength);
+        }
+        const int before = (int)wave_excl_scan((uint32_t)tiles, lane);
+        const unsigned long long past = __builtin_amdgcn_ballot_w64(before + tiles > unit);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            r.b = base + at;
+            r.place = (unit - __builtin_amdgcn_readlane(before, at)) * p.per_tile;
+        } else {
+            unit -= __builtin_amdgcn_readlane(before + tiles, 63);
+        }
+    }
+    if (r.b < 0) return r;
+    r.start = uniform(p.starts[r.b]);
+    r.fresh = uniform(p.starts[r.b + 1]) - r.start;
+    r.len = uniform(p.g.lens[r.b]);
+    if ((unsigned)r.len > (unsigned)p.g.max_pages * kPBT) {
+        r.bad = true;
+        if (lane == 0) flag(p.g.fault, kFaultLength);
+    } else if (r.len % kPBT && (unsigned)p.g.tails[r.b] >= (unsigned)p.g.n_tails) {
+        r.bad = true;
+        if (lane == 0) flag(p.g.fault, kFaultTail);
+    }
+    return r;
+}
+
+// Eight codes as fp16 times 2^k (`by`), exactly unless that is below fp16's smallest step.
+template <int C>
+__device__ __forceinline__ uint4 widen8_by(uint32_t a, uint32_t b, float by) {
+    half2v r[4];
+    if constexpr (C == kI8) {
+        a ^= 0x80808080u;
+        b ^= 0x80808080u;
+        const _Float16 f = (_Float16)by, o = (_Float16)(-1152.f * by);
+        const half2v ff = {f, f}, oo = {o, o};
+        r[0] = __builtin_elementwise_fma(__builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, a, 0x04010400u)), ff, oo);
+        r[1] = __builtin_elementwise_fma(__builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, a, 0x04030402u)), ff, oo);
+        r[2] = __builtin_elementwise_fma(__builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u)), ff, oo);
+        r[3] = __builtin_elementwise_fma(__builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u)), ff, oo);
+    } else {
+        r[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, by, false);
+        r[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, by, true);
+        r[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, false);
+        r[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, true);
+    }
+    return make_uint4(__builtin_bit_cast(uint32_t, r[0]), __builtin_bit_cast(uint32_t, r[1]), __builtin_bit_cast(uint32_t, r[2]),
+                      __builtin_bit_cast(uint32_t, r[3]));
+}
+
+// The LDS tiles in units of 16 bytes (eight fp16 values): K [64 tokens][D], V [D][64 tokens]; the units of a row change places so
+// that sixteen rows' units of one number hit sixteen different places of 256 bytes.
+template <int D>
+__device__ __forceinline__ int k_unit(int token, int chunk) {
+    if constexpr (D == 128) return token * 16 + (chunk ^ (token & 15));
+    else return token * 8 + (chunk ^ ((token >> 1) & 7));
+}
+__device__ __forceinline__ int v_unit(int channel, int chunk) { return channel * 8 + (chunk ^ ((channel >> 1) & 7)); }
+
+// What a wave has gathered for its 32 rows; lane (n, half) has row n.
+template <int D>
+struct RowState {
+    float16v o[D / 32];
+    float ref, sum;
+};
+
+template <int T, int D>
+__device__ __forceinline__ void store_rows(uint16_t *out, int half, const RowState<D> &st, float f) {
+#pragma unroll
+    for (int c = 0; c < D / 32; c++)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<uint2 *>(out + 32 * c + 2 * i + 4 * half) =
+                make_uint2(narrow2<T>(st.o[c][i] * f, st.o[c][i + 1] * f), narrow2<T>(st.o[c][i + 2] * f, st.o[c][i + 3] * f));
+}
+
+template <int T, int C, int D>
+__global__ __launch_bounds__(kPreThreads, 2) void paged_prefill_kernel(PrefillArgs p) {
+    constexpr int kUnits = kPBT * D / 8, kPieces = kPBT * D / 16 / kPreThreads;  // 16-byte units of a tile; pieces of 16 codes per thread
+    extern __shared__ __align__(16) uint4 s_tiles[];  // [2 buffers][K, V][kUnits]
+    __shared__ uint32_t s_big[2][kPreWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n = lane & 31, half = lane >> 5;
+    const int h = blockIdx.x % p.g.H, rest = blockIdx.x / p.g.H, split = rest % p.splits, unit = p.units - 1 - rest / p.splits;
+    const RowTile rt = find_tile(p, unit, lane);
+    if (rt.b < 0) return;
+    const int G = p.g.G, r = 32 * wave + n, place = rt.place + r / G, head = h * G + r % G;
+    const bool live = r < p.per_tile * G && place < rt.fresh;
+    const int past = rt.len - rt.fresh;
+    const int pos = live ? past + place : -1;
+    const int last_pos = past + min(rt.place + p.per_tile, rt.fresh) - 1;  // of the tile's last row
+    const int first_pos = past + rt.place;
+    // blocks that any row sees, and this workgroup's share of them
+    const int from = p.a.window > 0 && first_pos >= p.a.window ? (first_pos - p.a.window + 1) / kPBT : 0;
+    const int blocks = rt.bad || last_pos < 0 ? 0 : last_pos / kPBT + 1 - from;
+    const int t0 = from + (int)((long long)blocks * split / p.splits), t1 = from + (int)((long long)blocks * (split + 1) / p.splits);
+
+    constexpr int KS = D / 16;
+    half8v qf[KS];
+    float q_factor = fabsf(p.a.scale);
+    {
+        const uint16_t *q = p.a.q + (size_t)(rt.start + place) * p.a.q_stride + (size_t)head * D + 8 * half;
+        const uint32_t turn = p.a.scale < 0.f ? 0x80008000u : 0u;
+        uint4 w[KS];
+#pragma unroll
+        for (int k = 0; k < KS; k++) {
+            w[k] = live ? *reinterpret_cast<const uint4 *>(q + 16 * k) : make_uint4(0, 0, 0, 0);
+            w[k] = make_uint4(w[k].x ^ turn, w[k].y ^ turn, w[k].z ^ turn, w[k].w ^ turn);
+        }
+        if constexpr (T == kBF16) {
+            uint32_t big = 0;
+#pragma unroll
+            for (int k = 0; k < KS; k++) big = bf16_largest(bf16_largest(bf16_largest(bf16_largest(big, w[k].x), w[k].y), w[k].z), w[k].w);
+            const auto both = __builtin_amdgcn_permlane32_swap(big, big, false, false);
+            const int shift = bf16_shift(max(both[0], both[1]));
+            q_factor = ldexpf(q_factor, -shift);
+#pragma unroll
+            for (int k = 0; k < KS; k++)
+                w[k] = make_uint4(bf16_to_half2(w[k].x, shift), bf16_to_half2(w[k].y, shift), bf16_to_half2(w[k].z, shift),
+                                  bf16_to_half2(w[k].w, shift));
+        }
+#pragma unroll
+        for (int k = 0; k < KS; k++) qf[k] = __builtin_bit_cast(half8v, w[k]);
+    }
+    RowState<D> st;
+#pragma unroll
+    for (int c = 0; c < D / 32; c++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) st.o[c][i] = 0.f;
+    st.ref = -INFINITY;
+    st.sum = 0.f;
+    int e_ref = -10000;  // the accumulators are in units of 2^e_ref
+
+    uint4 ck[kPieces], cv[kPieces];
+    float ks = 0.f, vs = 0.f;
+    const int32_t *pages = p.g.table + (size_t)rt.b * p.g.max_pages;
+    const int unfinished = rt.len / kPBT;  // this block is in 16 bits
+    auto fetch = [&](int t) {
+        if (t >= t1 || t == unfinished) return;
+        int page = uniform(pages[t]);
+        const bool ok = (unsigned)page < (unsigned)p.g.n_pages;
+        if (!ok) {
+            if (tid == 0) flag(p.g.fault, kFaultPage);
+            page = 0;
+        }
+        const size_t tile = (size_t)page * p.g.H + h;
+        const uint4 *k = reinterpret_cast<const uint4 *>(p.g.k_codes + tile * kPBT * D), *v = reinterpret_cast<const uint4 *>(p.g.v_codes + tile * kPBT * D);
+#pragma unroll
+        for (int i = 0; i < kPieces; i++) ck[i] = k[tid + i * kPreThreads];
+#pragma unroll
+        for (int i = 0; i < kPieces; i++) cv[i] = v[tid + i * kPreThreads];
+        ks = ok ? p.g.scales[tile * 2] : __builtin_nanf("");
+        vs = p.g.scales[tile * 2 + 1];
+    };
+    fetch(t0);
+    // the last key that this wave's rows see, and the first
+    const int wave_last = past + min(rt.place + min(32 * wave + 31, p.per_tile * G - 1) / G, rt.fresh - 1);
+    const bool wave_live = 32 * wave < p.per_tile * G && rt.place + 32 * wave / G < rt.fresh;
+    const int wave_first = past + rt.place + 32 * wave / G;
+
+    for (int t = t0; t < t1; t++) {
+        uint4 *sk = s_tiles + (t & 1) * 2 * kUnits, *sv = sk + kUnits;
+        float k_scale = ks, v_mant = 1.f;
+        int e;
+        if (t != unfinished) {
+            e = vs > 0.f ? (int)(__float_as_uint(vs) >> 23) - 127 : -127;
+            if (e > -127) v_mant = ldexpf(vs, -e);
+            else if (vs > 0.f) { e = ilogbf(vs); v_mant = ldexpf(vs, -e); }
+            const int top = max(e, e_ref);
+            const float by = e - top < -24 && C == kI8 ? 0.f : ldexpf(1.f, max(e - top, -100));
+#pragma unroll
+            for (int i = 0; i < kPieces; i++) {
+                const int piece = tid + i * kPreThreads;
+                const int token = piece / (D / 16), chunk = piece % (D / 16) * 2;
+                sk[k_unit<D>(token, chunk)] = widen8_by<C>(ck[i].x, ck[i].y, 1.f);
+                sk[k_unit<D>(token, chunk + 1)] = widen8_by<C>(ck[i].z, ck[i].w, 1.f);
+                const int channel = piece / 4, part = piece % 4 * 2;
+                sv[v_unit(channel, part)] = widen8_by<C>(cv[i].x, cv[i].y, by);
+                sv[v_unit(channel, part + 1)] = widen8_by<C>(cv[i].z, cv[i].w, by);
+            }
+        } else {
+            // the block that is still in 16 bits: K as it is (bf16: times a power of two), V turned and brought to the accumulators' unit
+            const int count = rt.len - unfinished * kPBT;
+            const size_t at = ((size_t)uniform(p.g.tails[rt.b]) * p.g.H + h) * kPBT * D;
+            constexpr int kRowUnits = D / 8, kMine = kUnits / kPreThreads;
+            uint4 wk[kMine], wv[kMine];
+            uint32_t bk = 0, bv = 0;
+#pragma unroll
+            for (int i = 0; i < kMine; i++) {
+                const int u = tid + i * kPreThreads, token = u / kRowUnits;
+                wk[i] = wv[i] = make_uint4(0, 0, 0, 0);
+                if (token < count) {
+                    wk[i] = *reinterpret_cast<const uint4 *>(p.g.k_tail + at + (size_t)u * 8);
+                    wv[i] = *reinterpret_cast<const uint4 *>(p.g.v_tail + at + (size_t)u * 8);
+                }
+            }
+            auto largest = [](uint32_t m, uint32_t w) {
+                const uint32_t lo = w & 0x7fffu, hi = (w >> 16) & 0x7fffu;
+                m = lo < kInfBits<T> && lo > m ? lo : m;
+                return hi < kInfBits<T> && hi > m ? hi : m;
+            };
+#pragma unroll
+            for (int i = 0; i < kMine; i++) {
+                bk = largest(largest(largest(largest(bk, wk[i].x), wk[i].y), wk[i].z), wk[i].w);
+                bv = largest(largest(largest(largest(bv, wv[i].x), wv[i].y), wv[i].z), wv[i].w);
+            }
+            for (int x = 1; x < 64; x <<= 1) {
+                bk = max(bk, (uint32_t)__shfl_xor((int)bk, x));
+                bv = max(bv, (uint32_t)__shfl_xor((int)bv, x));
+            }
+            if (lane == 0) {
+                s_big[0][wave] = bk;
+                s_big[1][wave] = bv;
+            }
+            __syncthreads();
+            for (int i = 0; i < kPreWaves; i++) {
+                bk = max(bk, s_big[0][i]);
+                bv = max(bv, s_big[1][i]);
+            }
+            // the largest V to 2^14 .. 2^15; in fp16 the exponent of subnormal magnitudes counts as the smallest normal one
+            const int shift_k = T == kBF16 ? bf16_shift(bk) : 0;
+            const int shift_v = T == kBF16 ? bf16_shift(bv) : 29 - (int)max(bv >> 10, 1u);
+            k_scale = ldexpf(1.f, -shift_k);
+            e = -shift_v;
+            const int down = e - max(e, e_ref) + shift_v;
+#pragma unroll
+            for (int i = 0; i < kMine; i++) {
+                const int u = tid + i * kPreThreads, token = u / kRowUnits, chunk = u % kRowUnits;
+                uint32_t x[4] = {wk[i].x, wk[i].y, wk[i].z, wk[i].w};
+                if constexpr (T == kBF16) {
+#pragma unroll
+                    for (int c = 0; c < 4; c++) x[c] = bf16_to_half2(x[c], shift_k);
+                }
+                sk[k_unit<D>(token, chunk)] = make_uint4(x[0], x[1], x[2], x[3]);
+                const uint32_t y[4] = {wv[i].x, wv[i].y, wv[i].z, wv[i].w};
+#pragma unroll
+                for (int c = 0; c < 8; c++) {
+                    const float v = c & 1 ? wide_hi<T>(y[c >> 1]) : wide_lo<T>(y[c >> 1]);
+                    reinterpret_cast<_Float16 *>(sv + v_unit(8 * chunk + c, token >> 3))[token & 7] = (_Float16)ldexpf(v, down);
+                }
+            }
+        }
+        fetch(t + 1);
+        __syncthreads();
+        const float by_e = e > e_ref ? ldexpf(1.f, max(e_ref - e, -200)) : 1.f;  // the accumulators to a larger unit
+        e_ref = max(e_ref, e);
+        const bool skip = !wave_live || t * kPBT > wave_last || (p.a.window > 0 && t * kPBT + kPBT - 1 <= wave_first - p.a.window);
+        if (skip) {
+            if (by_e != 1.f) {
+#pragma unroll
+                for (int c = 0; c < D / 32; c++) st.o[c] *= by_e;
+            }
+            continue;
+        }
+
+        float16v s[2];
+        const int token = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
+#pragma unroll
+        for (int j = 0; j < 2; j++) {
+#pragma unroll
+            for (int i = 0; i < 16; i++) s[j][i] = 0.f;
+#pragma unroll
+            for (int k = 0; k < KS; k++)
+                s[j] = mfma32(__builtin_bit_cast(half8v, sk[k_unit<D>(32 * j + token, 2 * k + half)]), qf[k], s[j]);
+        }
+        const float f = k_scale * q_factor;
+        const bool masked = t * kPBT + kPBT - 1 > wave_first || (p.a.window > 0 && t * kPBT <= wave_last - p.a.window);
+        const int low = p.a.window > 0 ? pos - p.a.window : -1;
+        auto hidden = [&](int j, int i) {
+            const int key = t * kPBT + 32 * j + 16 * (i >> 3) + 8 * half + (i & 7);
+            return key > pos || key <= low;
+        };
+        float mx = -INFINITY;
+        if (masked) {
+#pragma unroll
+            for (int j = 0; j < 2; j++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) mx = fmaxf(mx, hidden(j, i) ? -INFINITY : s[j][i]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 2; j++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) mx = fmaxf(mx, s[j][i]);
+        }
+        {
+            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+            mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * f;
+        }
+        const bool move = mx - st.ref > kRefMost;
+        if (__builtin_amdgcn_ballot_w64(move) || by_e != 1.f) {
+            const float ref = move ? fmaxf(mx, kLowestRef) - kRefLead : st.ref;
+            const float alpha = move ? __builtin_amdgcn_exp2f(st.ref - ref) : 1.f;
+            st.ref = ref;
+            st.sum *= alpha;
+#pragma unroll
+            for (int c = 0; c < D / 32; c++) st.o[c] *= alpha * by_e;
+        }
+        const float mant = __builtin_amdgcn_logf(v_mant), off = mant - st.ref;
+        uint32_t pw[2][8];
+        float sum = 0.f;
+        const half2v ones = {(_Float16)1.f, (_Float16)1.f};
+#pragma unroll
+        for (int j = 0; j < 2; j++)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                float a = __builtin_amdgcn_exp2f(fmaf(s[j][i], f, off)), b = __builtin_amdgcn_exp2f(fmaf(s[j][i + 1], f, off));
+                if (masked) {
+                    a = hidden(j, i) ? 0.f : a;
+                    b = hidden(j, i + 1) ? 0.f : b;
+                }
+                pw[j][i >> 1] = narrow2<kF16>(a, b);
+                sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, pw[j][i >> 1]), ones, sum, false);
+            }
+        st.sum = fmaf(sum, __builtin_amdgcn_exp2f(-mant), st.sum);
+#pragma unroll
+        for (int x = 0; x < 4; x++) {
+            const uint32_t *w = pw[x >> 1] + 4 * (x & 1);
+            const half8v pf = __builtin_bit_cast(half8v, make_uint4(w[0], w[1], w[2], w[3]));
+#pragma unroll
+            for (int c = 0; c < D / 32; c++)
+                st.o[c] = mfma32(__builtin_bit_cast(half8v, sv[v_unit(32 * c + n, 2 * x + half)]), pf, st.o[c]);
+        }
+    }
+
+    float sum;
+    {
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(st.sum), __float_as_uint(st.sum), false, false);
+        sum = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+    }
+    e_ref = max(e_ref, -140);  // still there where nothing was met
+    if (p.splits == 1) {
+        if (!live) return;
+        const float f = rt.bad ? __builtin_nanf("") : sum == 0.f ? 0.f : 1.f / sum, unit_v = ldexpf(1.f, e_ref);
+#pragma unroll
+        for (int c = 0; c < D / 32; c++) st.o[c] *= f;  // first: with their unit they could be too large
+        store_rows<T, D>(p.a.out + (size_t)(rt.start + place) * p.a.out_stride + (size_t)head * D, half, st, unit_v);
+        return;
+    }
+    float *part = p.a.partials + (((size_t)(unit * p.g.H + h) * p.splits + split) * kPreRows + r) * partial_pitch(D);
+    if (!live) return;
+#pragma unroll
+    for (int c = 0; c < D / 32; c++)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<float4 *>(part + 32 * c + 2 * i + 4 * half) =
+                make_float4(st.o[c][i], st.o[c][i + 1], st.o[c][i + 2], st.o[c][i + 3]);
+    if (half == 0) {
+        part[D] = st.ref;
+        part[D + 1] = rt.bad ? __builtin_nanf("") : sum;
+        part[D + 2] = (float)e_ref;
+    }
+}
+
+// Joins the splits of a row tile: one wave per row, D / 64 channels a lane.
+constexpr int kJoinRows = 16;
+template <int T, int D>
+__global__ __launch_bounds__(256) void paged_join_kernel(PrefillArgs p) {
+    constexpr int kJoinGroups = kPreRows / kJoinRows;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int group = blockIdx.x % kJoinGroups, rest = blockIdx.x / kJoinGroups, h = rest % p.g.H, unit = rest / p.g.H;
+    const RowTile rt = find_tile(p, unit, lane);
+    if (rt.b < 0) return;
+    for (int r = group * kJoinRows + wave; r < (group + 1) * kJoinRows; r += 4) {
+        const int place = rt.place + r / p.g.G;
+        if (r >= p.per_tile * p.g.G || place >= rt.fresh) return;
+        const float *part = p.a.partials + ((size_t)(unit * p.g.H + h) * p.splits * kPreRows + r) * partial_pitch(D);
+        const size_t step = (size_t)kPreRows * partial_pitch(D);
+        float top = -INFINITY, e_top = -140.f;
+        for (int s = 0; s < p.splits; s++) {
+            top = fmaxf(top, part[s * step + D]);
+            e_top = fmaxf(e_top, part[s * step + D + 2]);
+        }
+        float sum = 0.f, o[D / 64];
+#pragma unroll
+        for (int c = 0; c < D / 64; c++) o[c] = 0.f;
+        for (int s = 0; s < p.splits; s++) {
+            const float m = part[s * step + D], l = part[s * step + D + 1];
+            const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+            sum += m == -INFINITY ? (l != l ? l : 0.f) : l * f;  // a split that met nothing takes no part
+            const float fo = f * __builtin_amdgcn_exp2f(part[s * step + D + 2] - e_top);
+#pragma unroll
+            for (int c = 0; c < D / 64; c++) o[c] = fmaf(part[s * step + lane * (D / 64) + c], fo, o[c]);
+        }
+        const float f = sum == 0.f ? 0.f : 1.f / sum, unit_v = ldexpf(1.f, (int)e_top);
+        uint16_t *out = p.a.out + (size_t)(rt.start + place) * p.a.out_stride + (size_t)(h * p.g.G + r % p.g.G) * D + lane * (D / 64);
+        if constexpr (D == 128) *reinterpret_cast<uint32_t *>(out) = narrow2<T>(o[0] * f * unit_v, o[1] * f * unit_v);
+        else *out = (uint16_t)narrow2<T>(o[0] * f * unit_v, 0.f);
+    }
+}
+
+template <int T, int C, int D>
+hipError_t launch(PrefillArgs p, int max_len, hipStream_t s) {
+    constexpr size_t kLds = (size_t)4 * kPBT * D * 2;
+    auto kernel = paged_prefill_kernel<T, C, D>;
+    static std::atomic<uint64_t> allowed{0};
+    hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), kLds, allowed);
+    if (e != hipSuccess) return e;
+    p.per_tile = kPreRows / p.g.G;
+    // every sequence has at most one row tile that is not full
+    p.units = p.n_tokens / p.per_tile + (p.g.batch < p.n_tokens ? p.g.batch : p.n_tokens);
+    const long long base = (long long)p.units * p.g.H, pages = max_len > 0 && max_len < p.g.max_pages * kPBT ? (max_len + kPBT - 1) / kPBT : p.g.max_pages;
+    p.splits = (int)std::max(1ll, std::min((long long)kPrefillSplitWGs / base, pages / 8));
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(base * p.splits)), dim3(kPreThreads), kLds, s, p);
+    if (p.splits > 1)
+        hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3((unsigned)(base * (kPreRows / kJoinRows))), dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_prefill(const PagedGeo &g, const PagedAttn &a, const int32_t *starts, int n_tokens, int max_new, int max_len,
+                                int head_dim, int data_type, int code_type, hipStream_t s) {
+    (void)max_new;
+    PrefillArgs p = {g, a, n_tokens, 0, 0, 0, starts};
+    auto by_dim = [&](auto t, auto c) {
+        if (head_dim == 64) return launch<decltype(t)::value, decltype(c)::value, 64>(p, max_len, s);
+        return launch<decltype(t)::value, decltype(c)::value, 128>(p, max_len, s);
+    };
+    auto by_code = [&](auto t) {
+        if (code_type == kI8) return by_dim(t, std::integral_constant<int, kI8>());
+        return by_dim(t, std::integral_constant<int, kE4M3>());
+    };
+    if (data_type == kF16) return by_code(std::integral_constant<int, kF16>());
+    return by_code(std::integral_constant<int, kBF16>());
+}
+
+}  // namespace kvc

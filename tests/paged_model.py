@@ -97,14 +97,15 @@ def check_stored(cache, seqs, table, tails, lens):
 
 
 def attention(q, k, v, scale, pos, window):
-    """q [rows, Hq, D] at positions pos [rows] over k, v [length, H, D], float64: out, and the mean of |v| under the weights."""
+    """q [rows, Hq, D] at positions pos [rows] over k, v [length, H, D], float64: out, the mean of |v| under the weights,
+    the largest sum of magnitudes that a score is made of, and the sum of |v| over the keys that a row sees."""
     rows, Hq, D = q.shape
     H = k.shape[1]
     G = Hq // H
     out, size = torch.zeros((rows, Hq, D), dtype=F64), torch.zeros((rows, Hq, D), dtype=F64)
-    spread = torch.zeros((rows, Hq, 1), dtype=F64)
+    spread, plain = torch.zeros((rows, Hq, 1), dtype=F64), torch.zeros((rows, Hq, D), dtype=F64)
     if k.shape[0] == 0:
-        return out, size, spread
+        return out, size, spread, plain
     j = torch.arange(k.shape[0])
     seen = j <= pos[:, None]
     if window:
@@ -117,6 +118,6 @@ def attention(q, k, v, scale, pos, window):
         p = torch.softmax(s, dim=-1)
         p = torch.where(any_[:, None], p, torch.zeros_like(p))
         vv = torch.where(seen.any(0)[:, None], v[:, g // G], torch.zeros_like(v[:, g // G]))
-        out[:, g], size[:, g] = p @ vv, p @ vv.abs()
+        out[:, g], size[:, g], plain[:, g] = p @ vv, p @ vv.abs(), seen.double() @ vv.abs()
         spread[:, g, 0] = torch.where(seen & torch.isfinite(mass), mass, torch.zeros_like(mass)).amax(1)
-    return out, size, spread
+    return out, size, spread, plain

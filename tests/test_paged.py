@@ -310,7 +310,7 @@ def test_append_captured_and_replayed(gpu):
         w.check()
 
 
-def _close(got, ref, size, spread, dtype):
+def _close(got, ref, size, spread, plain, dtype):
     """Attention's outputs against 64 bits.  The output is rounded once: eps / 2 of its value (or half the type's smallest step).
     A score is off by what 128 or fewer products summed in binary32 and two or three factors lose, (128 + 8) * 2^-24 of the sum of
     their magnitudes `spread` (bf16 in fp16 parts adds 2^-40 of the largest); numerators and denominator change by that share, and by
@@ -326,15 +326,15 @@ def _close(got, ref, size, spread, dtype):
 
 def _reference(w, rows, window, scale, q):
     """Model attention of the last rows[b] tokens of every sequence over what the cache holds; q rows one after the other."""
-    out, size, spread, at = [], [], [], 0
+    parts, at = [[], [], [], []], 0
     now = M.Snapshot(w.cache)
     for b, n in enumerate(rows):
         k, v = now.held(w.table[b], w.tails[b], w.lens[b])
         pos = torch.arange(w.lens[b] - n, w.lens[b])
-        for got, x in zip((out, size, spread), M.attention(q[at:at + n].double(), k, v, scale, pos, window)):
+        for got, x in zip(parts, M.attention(q[at:at + n].double(), k, v, scale, pos, window)):
             got.append(x)
         at += n
-    return torch.cat(out), torch.cat(size), torch.cat(spread)
+    return [torch.cat(x) for x in parts]
 
 
 def _decode(w, q_len, window=0, scale=None, **kw):
@@ -342,8 +342,8 @@ def _decode(w, q_len, window=0, scale=None, **kw):
     scale = 1 / math.sqrt(w.D) if scale is None else scale
     got = w.cache.attn_decode(q.cuda(), scale, _i32(w.lens), w.d_table, w.d_tails, q_len=q_len, window=window, **kw)
     torch.cuda.synchronize()
-    ref, size, spread = _reference(w, [q_len] * w.batch, window, scale, q)
-    _close(got, ref, size, spread, w.dtype)
+    want64 = _reference(w, [q_len] * w.batch, window, scale, q)
+    _close(got, *want64, w.dtype)
     return q, got
 
 
@@ -420,8 +420,8 @@ def test_decode_large_and_small_values(gpu, dtype, codes):
     _decode(w, 1, scale=0.0)
     q = torch.zeros((4, 4, 128), dtype=dtype, device="cuda:0")
     got = w.cache.attn_decode(q, 1.0, _i32(w.lens), w.d_table, w.d_tails)
-    ref, size, spread = _reference(w, [1] * 4, 0, 1.0, q.cpu())
-    _close(got, ref, size, spread, dtype)
+    want64 = _reference(w, [1] * 4, 0, 1.0, q.cpu())
+    _close(got, *want64, dtype)
 
 
 @pytest.mark.parametrize("D", [64, 128])
@@ -508,3 +508,229 @@ def test_decode_shared_pages_other_streams_and_replays(gpu):
         assert torch.equal(out, eager)
         if not shorter:
             assert torch.equal(out, want)
+
+
+def _starts(counts):
+    return _i32(list(itertools.accumulate([0] + list(counts))))
+
+
+def _close_chunks(got, ref, size, spread, plain, dtype):
+    """As _close, but the weights go into the second product with fp16's 11 bits: each is off by at most 2^-11 of itself, and so
+    is the sum that they are divided by, which is taken from the same rounded ones: 2 * 2^-11 of the weighted magnitudes at
+    most.  fp16's smallest step is 2^-24, and the reference leaves a row's largest weight at 2^8 at least: half a step is 2^-33 of
+    the sum of the weights, for every key that is seen, so 2^-33 of the sum of their magnitudes `plain`.  In the same way the codes
+    of a block whose V scale is far below the largest so far are off by half a step of 2^-24 against codes of up to 2^7, at most
+    2^-32 of the largest magnitude, under weights whose sum is one; a code is at most 448 / 2^-9 = 2^18 times another of its
+    block, and 2^-32 of the largest is within 2^-32 of `plain`.  The first two powers together: 2^-31 of `plain`."""
+    got = got.cpu().double()
+    eps = torch.finfo(dtype).eps / 2
+    share = 2 * 136 * 2.0 ** -24 * spread + 2 * 2.0 ** -11 + 2 * 64 * 2.0 ** -24
+    tol = eps * ref.abs() + share * size * (1 + eps) + (2.0 ** -25 if dtype is torch.float16 else 2.0 ** -134)
+    tol = tol + 2.0 ** -31 * plain.amax(dim=-1, keepdim=True)
+    err = (got - ref).abs()
+    assert bool((err <= tol).all()), (float((err - tol).max()), float((err / tol).max()))
+
+
+def _prefill(w, rows, window=0, scale=None, **kw):
+    n = sum(rows)
+    q = w.rand(n + 3, w.Hq, w.D).to(w.dtype)
+    scale = 1 / math.sqrt(w.D) if scale is None else scale
+    out = torch.full(q.shape, 7.0, dtype=w.dtype, device="cuda:0")
+    w.cache.attn_prefill(q.cuda(), scale, _starts(rows), _i32(w.lens), w.d_table, w.d_tails, window=window, out=out, **kw)
+    torch.cuda.synchronize()
+    want64 = _reference(w, rows, window, scale, q)
+    _close_chunks(out[:n], *want64, w.dtype)
+    assert (out[n:] == 7).all()
+    return q, out
+
+
+@pytest.mark.parametrize("dtype,codes", TYPES, ids=IDS)
+@pytest.mark.parametrize("H,G,D", [(1, 1, 128), (2, 8, 128), (3, 3, 64), (2, 4, 64), (1, 32, 128), (8, 5, 64)])
+def test_prefill(gpu, dtype, codes, H, G, D):
+    """Ragged chunks behind pasts of all lengths, chunks of nothing, of one token, of several row tiles."""
+    w = World(gpu, 7, H, G, D, dtype, codes, 10, seed=H * G + D)
+    first = [0, 64, 63, 1, 130, 0, 100]
+    k, v, _ = w.tokens(sum(first))
+    w.append(first, k, v)
+    rows = [200, 64, 1, 0, 70, 1, 333]
+    k, v, _ = w.tokens(sum(rows))
+    w.append(rows, k, v)
+    _prefill(w, rows, max_new=333, max_len=433)
+    _prefill(w, rows)
+    _prefill(w, rows, scale=-0.2)
+    w.cache.check()
+
+
+@pytest.mark.parametrize("window", [1, 2, 63, 64, 65, 100, 1000, 1 << 30])
+def test_prefill_sliding_window(gpu, window):
+    for dtype, codes, D in ((torch.float16, "int8", 64), (torch.bfloat16, "e4m3", 128)):
+        w = World(gpu, 4, 2, 3, D, dtype, codes, 8, seed=window % 91)
+        rows = [500, 1, 130, 64]
+        k, v, _ = w.tokens(sum(rows))
+        w.append(rows, k, v)
+        _prefill(w, rows, window)
+
+
+@pytest.mark.parametrize("batch,H,G,past,new", [(1, 1, 1, 8000, 20), (1, 2, 8, 4000, 3), (2, 1, 4, 3000, 40), (1, 1, 2, 1000, 700), (3, 2, 1, 2000, 1)])
+def test_prefill_few_rows_over_a_long_past(gpu, batch, H, G, past, new):
+    """The keys are split among workgroups; the same bits twice."""
+    for D in (64, 128):
+        w = World(gpu, batch, H, G, D, torch.float16, "e4m3", (past + new) // 64 + 1, seed=past)
+        counts = [past] + [past // 3] * (batch - 1)
+        k, v, _ = w.tokens(sum(counts))
+        w.append(counts, k, v)
+        k, v, _ = w.tokens(new * batch)
+        w.append([new] * batch, k, v)
+        q, a = _prefill(w, [new] * batch)
+        b = w.cache.attn_prefill(q.cuda(), 1 / math.sqrt(D), _starts([new] * batch), _i32(w.lens), w.d_table, w.d_tails, max_new=new)
+        assert torch.equal(a[:new * batch], b[:new * batch])
+        _prefill(w, [new] * batch, window=500)
+
+
+@pytest.mark.parametrize("dtype,codes", TYPES, ids=IDS)
+def test_prefill_large_and_small_values(gpu, dtype, codes):
+    """Blocks whose V scales lie far apart, growing and falling, scores far apart, zeros."""
+    w = World(gpu, 3, 1, 2, 128, dtype, codes, 5, seed=3)
+    k, v, _ = w.tokens(3 * 300)
+    steps = [1, 1e-3, 30, 1e-2, 300]
+    for j, f in enumerate(steps):
+        v[64 * j:64 * j + 64] = (v[64 * j:64 * j + 64].double() * f).to(dtype)
+        v[600 + 64 * j:664 + 64 * j] = (v[600 + 64 * j:664 + 64 * j].double() * steps[4 - j]).to(dtype)
+    k[300:600] = (k[300:600].double() * 30).to(dtype)
+    v[364:428], k[428:492] = 0, 0
+    w.append([300] * 3, k, v)
+    _prefill(w, [300] * 3)
+    _prefill(w, [7] * 3)
+    _prefill(w, [300] * 3, scale=0.0)
+
+
+def test_attention_at_the_ends_of_the_range_of_bf16(gpu):
+    w = World(gpu, 2, 1, 1, 64, torch.bfloat16, "int8", 3, seed=3)
+    k, v, _ = w.tokens(2 * 150)
+    v[:150] = (v[:150].sign().double() * 3e38).to(torch.bfloat16)
+    v[150:] = (v[150:].double() * 1e-28).to(torch.bfloat16)
+    w.append([150, 150], k, v)
+    _decode(w, 1)
+    _prefill(w, [150, 150])
+    _prefill(w, [3, 3])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype,codes", TYPES, ids=IDS)
+def test_prefill_non_finite_tokens_reach_only_the_rows_that_see_them(gpu, dtype, codes, D):
+    w = World(gpu, 2, 2, 1, D, dtype, codes, 4, seed=4)
+    rows = [200, 100]
+    k, v, q = w.tokens(300)
+    v[70, 1, 5] = math.inf          # sequence 0, block 1, head 1
+    k[200 + 98, 0, 7] = math.nan    # sequence 1, unfinished block
+    v[200 + 99, 1, 0] = -math.inf
+    w.append(rows, k, v)
+    for window in (0, 80):
+        got = w.cache.attn_prefill(q.cuda(), 0.1, _starts(rows), _i32(w.lens), w.d_table, w.d_tails, window=window).cpu()
+        want = torch.zeros(got.shape, dtype=torch.bool)
+        want[64:200, 1] = True   # a block's scale stands for all of its tokens
+        if window:
+            want[127 + window:200, 1] = False
+        want[200 + 98:, 0] = True
+        want[200 + 99:, 1] = True
+        assert torch.equal(torch.isnan(got), want), window
+
+
+def test_prefill_empty_rows_and_places_out_of_range(gpu):
+    """More rows than a length has tokens: zeros for those before the beginning.  Pages, tails, lengths that do not fit: NaN.
+    Starts that do not fit: rows left as they were."""
+    w = World(gpu, 3, 2, 2, 64, torch.bfloat16, "int8", 3, seed=6)
+    k, v, _ = w.tokens(300)
+    w.append([100] * 3, k, v)
+    rows = [100, 100, 100]
+    q, want = _prefill(w, rows)
+    more = [110, 100, 3]
+    q2 = w.rand(213, 4, 64).to(torch.bfloat16)
+    got = w.cache.attn_prefill(q2.cuda(), 1 / 8, _starts(more), _i32(w.lens), w.d_table, w.d_tails)
+    want64 = _reference(w, more, 0, 1 / 8, q2)
+    _close_chunks(got, *want64, w.dtype)
+    assert not got[:10].any()
+    got = w.cache.attn_prefill(q2.cuda(), 1 / 8, _starts(more), _i32([0, 100, 100]), w.d_table, w.d_tails)
+    assert not got[:110].any()
+    w.cache.check()
+    for what in ("page", "page_low", "tail", "length", "length_low", "starts", "starts_end", "starts_low"):
+        lens, table, tails, starts = list(w.lens), w.table.clone(), w.tails.clone(), [0, 100, 200, 300]
+        if what.startswith("page"):
+            table[1, 0] = -1 if what == "page_low" else w.cache.n_pages
+        elif what == "tail":
+            tails[1] = w.cache.n_tails
+        elif what.startswith("length"):
+            lens[1] = -1 if what == "length_low" else 193
+        elif what == "starts":
+            starts = [0, 200, 100, 200]
+        elif what == "starts_end":
+            starts = [0, 100, 200, 304]
+        else:
+            starts = [-1, 99, 200, 300]
+        out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda:0")
+        w.cache.attn_prefill(q.cuda(), 1 / 8, _i32(starts), _i32(lens), _i32(table), _i32(tails), out=out)
+        with pytest.raises(gpu.KvcompError) as e:
+            w.cache.check()
+        assert e.value.status == gpu.ERR_STATE, what
+        if what == "starts_end":
+            assert torch.equal(out[:200], want[:200]) and (out[200:] == 7).all()
+        elif what == "starts_low":
+            assert (out[:99] == 7).all() and torch.equal(out[200:300], want[200:300])
+        elif not what.startswith("starts"):
+            assert torch.isnan(out[100:200]).all(), what
+            assert torch.equal(out[:100], want[:100]) and torch.equal(out[200:300], want[200:300]), what
+
+
+def test_a_prompt_a_chunk_and_steps_as_a_server_runs_them(gpu):
+    """Prompt, its attention, single steps that cross a block's end, a drafted step set back, a second chunk: every output against
+    the model, the decode steps captured once and replayed with the lengths of the day between eager calls."""
+    H, G, D = 2, 4, 128
+    w = World(gpu, 3, H, G, D, torch.bfloat16, "e4m3", 8, seed=12)
+    cos_sin = gpu.Rope.table(512, D).cpu()
+    rope, scale = (cos_sin, False, None, gpu), 1 / math.sqrt(D)
+
+    def chunk(counts):
+        k, v, q = w.tokens(sum(counts))
+        qr = w.append(counts, k, v, q, rope=rope)
+        got = w.cache.attn_prefill(qr, scale, _starts(counts), _i32(w.lens), w.d_table, w.d_tails, max_new=max(counts))
+        want64 = _reference(w, counts, 0, scale, qr.cpu())
+        _close_chunks(got, *want64, w.dtype)
+
+    chunk([190, 61, 5])
+    lens, one = _i32(w.lens), _i32([1, 1, 1])
+    dk, dv, dq = (torch.empty((3, n, D), dtype=w.dtype, device="cuda:0") for n in (H, H, H * G))
+    qr, out = torch.empty_like(dq), torch.empty_like(dq)
+    d_rope, ws = gpu.Rope(cos_sin.cuda()), w.cache.new_workspace()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        lens.add_(one)
+        w.cache.append(dk, dv, lens, w.d_table, w.d_tails, q=dq, q_out=qr, rope=d_rope)
+        w.cache.attn_decode(qr, scale, lens, w.d_table, w.d_tails, out=out, workspace=ws)
+    for step in range(5):
+        k, v, q = w.tokens(3)
+        pos = torch.tensor([w.lens])
+        w.lens = [x + 1 for x in w.lens]
+        kr, size = M.rotate(k.double(), cos_sin, pos)
+        for b in range(3):
+            w.seqs.add(b, [kr[b]], [size[b]], [v[b].double()])
+        for a, b in ((dk, k), (dv, v), (dq, q)):
+            a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        want64 = _reference(w, [1] * 3, 0, scale, qr.cpu())
+        _close(out, *want64, w.dtype)
+        assert torch.equal(out, w.cache.attn_decode(qr, scale, lens, w.d_table, w.d_tails))
+    w.check()
+    # four drafted tokens, two of them taken back (no block ends among them: 195, 66 and 10 tokens)
+    k, v, q = w.tokens(12)
+    qr4 = w.append([4, 4, 4], k, v, q, rope=rope)
+    got = w.cache.attn_decode(qr4, scale, _i32(w.lens), w.d_table, w.d_tails, q_len=4)
+    want64 = _reference(w, [4] * 3, 0, scale, qr4.cpu())
+    _close(got, *want64, w.dtype)
+    w.lens = [x - 2 for x in w.lens]
+    for lists in (w.seqs.k, w.seqs.size, w.seqs.v):
+        for x in lists:
+            del x[-2:]
+    chunk([3, 100, 60])
+    w.check()

@@ -99,3 +99,71 @@ def test_null_structures(B):
         _refused(B, lib.kvcomp_paged_append(*args, None))
     _refused(B, lib.kvcomp_paged_check(None, None))
     _refused(B, lib.kvcomp_paged_check(_memory(B, d_fault=0), None))
+
+
+def _decode_args(B, **kw):
+    lib = B.load()
+    ws = lib.kvcomp_paged_workspace_bytes(_config(B))
+    d = dict(q=ALIGNED, q_stride=4096, q_len=1, scale=0.1, window=0, max_len=0, out=ALIGNED, out_stride=4096, ws=ALIGNED, ws_bytes=ws)
+    d.update(kw)
+    return [*d.values(), None]
+
+
+def _prefill_args(B, **kw):
+    lib = B.load()
+    ws = lib.kvcomp_paged_workspace_bytes(_config(B))
+    d = dict(q=ALIGNED, q_stride=4096, starts=ALIGNED, n_tokens=50, scale=0.1, window=0, max_new=0, max_len=0, out=ALIGNED,
+             out_stride=4096, ws=ALIGNED, ws_bytes=ws)
+    d.update(kw)
+    return [*d.values(), None]
+
+
+def test_workspace_size(B):
+    lib = B.load()
+    assert lib.kvcomp_paged_workspace_bytes(_config(B)) > lib.kvcomp_paged_workspace_bytes(_config(B, head_dim=64)) > 0
+    assert lib.kvcomp_paged_workspace_bytes(_config(B, head_dim=80)) == 0 and lib.kvcomp_paged_workspace_bytes(None) == 0
+
+
+@pytest.mark.parametrize("i", range(len(BAD_CONFIGS) + len(BAD_MEMORY) + len(BAD_BATCHES)))
+def test_attention_refuses_bad_caches(B, i):
+    bad = (BAD_CONFIGS + BAD_MEMORY + BAD_BATCHES)[i]
+    cfg, mem, seqs = _config(B), _memory(B), _batch(B)
+    if i < len(BAD_CONFIGS):
+        cfg = _config(B, **bad)
+    elif i < len(BAD_CONFIGS) + len(BAD_MEMORY):
+        mem = _memory(B, **bad)
+    else:
+        seqs = _batch(B, **bad)
+    _refused(B, B.load().kvcomp_paged_attn_decode(cfg, mem, seqs, *_decode_args(B)))
+    _refused(B, B.load().kvcomp_paged_attn_prefill(cfg, mem, seqs, *_prefill_args(B)))
+
+
+COMMON = [dict(q=0), dict(q=ALIGNED + 8), dict(q_stride=4088), dict(q_stride=4100), dict(out=0), dict(out=ALIGNED + 2), dict(out_stride=4000),
+          dict(scale=float("inf")), dict(scale=float("nan")), dict(window=-1), dict(max_len=-1), dict(ws=0), dict(ws=ALIGNED + 8)]
+
+
+@pytest.mark.parametrize("bad", COMMON + [dict(q_len=0), dict(q_len=-1), dict(q_len=9), dict(q_len=1 << 30)])
+def test_decode_refuses_bad_arguments(B, bad):
+    _refused(B, B.load().kvcomp_paged_attn_decode(_config(B), _memory(B), _batch(B), *_decode_args(B, **bad)))
+
+
+@pytest.mark.parametrize("bad", COMMON + [dict(starts=0), dict(starts=ALIGNED + 2), dict(n_tokens=-1), dict(n_tokens=1 << 26), dict(max_new=-1)])
+def test_prefill_refuses_bad_arguments(B, bad):
+    _refused(B, B.load().kvcomp_paged_attn_prefill(_config(B), _memory(B), _batch(B), *_prefill_args(B, **bad)))
+
+
+def test_attention_refuses_small_workspaces_and_large_batches(B):
+    lib = B.load()
+    small = lib.kvcomp_paged_workspace_bytes(_config(B)) - 1
+    assert lib.kvcomp_paged_attn_decode(_config(B), _memory(B), _batch(B), *_decode_args(B, ws_bytes=small)) == B.ERR_CAPACITY
+    assert lib.kvcomp_paged_attn_prefill(_config(B), _memory(B), _batch(B), *_prefill_args(B, ws_bytes=small)) == B.ERR_CAPACITY
+    _refused(B, lib.kvcomp_paged_attn_decode(_config(B), _memory(B), _batch(B, batch=4097), *_decode_args(B)))
+    _refused(B, lib.kvcomp_paged_attn_decode(_config(B, max_pages=1 << 20), _memory(B), _batch(B, batch=256), *_decode_args(B)))
+
+
+def test_nothing_to_attend_is_fine(B):
+    lib = B.load()
+    none = _batch(B, batch=0, d_lens=0, d_table=0, d_tails=0)
+    assert lib.kvcomp_paged_attn_decode(_config(B), _memory(B), none, *_decode_args(B, q=0, out=0)) == B.OK
+    assert lib.kvcomp_paged_attn_prefill(_config(B), _memory(B), none, *_prefill_args(B)) == B.OK
+    assert lib.kvcomp_paged_attn_prefill(_config(B), _memory(B), _batch(B), *_prefill_args(B, n_tokens=0, q=0)) == B.OK
