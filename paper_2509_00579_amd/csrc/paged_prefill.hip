@@ -61,11 +61,12 @@ __device__ __forceinline__ RowTile find_tile(const PrefillArgs &p, int unit, int
         if (past) {
             const int at = __builtin_ctzll(past);
             r.b = base + at;
-            r.place = (unit - __builtin_amdgcn_readlane(before, at)) * p.per_tile;
+            r.place = uniform(unit - __builtin_amdgcn_readlane(before, at)) * p.per_tile;
         } else {
             unit -= __builtin_amdgcn_readlane(before + tiles, 63);
         }
     }
+    r.b = uniform(r.b);
     if (r.b < 0) return r;
     r.start = uniform(p.starts[r.b]);
     r.fresh = uniform(p.starts[r.b + 1]) - r.start;
@@ -112,6 +113,19 @@ __device__ __forceinline__ int k_unit(int token, int chunk) {
 }
 __device__ __forceinline__ int v_unit(int channel, int chunk) { return channel * 8 + (chunk ^ ((channel >> 1) & 7)); }
 
+// The order of `count` products and the LDS reads of their left operands: four reads ahead, no more (left to itself the
+// compiler reads all of them first and runs out of registers).
+template <int count>
+__device__ __forceinline__ void ahead() {
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+    for (int i = 0; i < count - 4; i += 2) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+}
+
 // What a wave has gathered for its 32 rows; lane (n, half) has row n.
 template <int D>
 struct RowState {
@@ -135,7 +149,7 @@ __global__ __launch_bounds__(kPreThreads, 2) void paged_prefill_kernel(PrefillAr
     extern __shared__ __align__(16) uint4 s_tiles[];  // [2 buffers][K, V][kUnits]
     __shared__ uint32_t s_big[2][kPreWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n = lane & 31, half = lane >> 5;
-    const int h = blockIdx.x % p.g.H, rest = blockIdx.x / p.g.H, split = rest % p.splits, unit = p.units - 1 - rest / p.splits;
+    const int h = uniform(blockIdx.x % p.g.H), rest = uniform(blockIdx.x / p.g.H), split = uniform(rest % p.splits), unit = p.units - 1 - uniform(rest / p.splits);
     const RowTile rt = find_tile(p, unit, lane);
     if (rt.b < 0) return;
     const int G = p.g.G, r = 32 * wave + n, place = rt.place + r / G, head = h * G + r % G;
@@ -147,7 +161,7 @@ __global__ __launch_bounds__(kPreThreads, 2) void paged_prefill_kernel(PrefillAr
     // blocks that any row sees, and this workgroup's share of them
     const int from = p.a.window > 0 && first_pos >= p.a.window ? (first_pos - p.a.window + 1) / kPBT : 0;
     const int blocks = rt.bad || last_pos < 0 ? 0 : last_pos / kPBT + 1 - from;
-    const int t0 = from + (int)((long long)blocks * split / p.splits), t1 = from + (int)((long long)blocks * (split + 1) / p.splits);
+    const int t0 = uniform(from + (int)((long long)blocks * split / p.splits)), t1 = uniform(from + (int)((long long)blocks * (split + 1) / p.splits));
 
     constexpr int KS = D / 16;
     half8v qf[KS];
@@ -189,7 +203,7 @@ __global__ __launch_bounds__(kPreThreads, 2) void paged_prefill_kernel(PrefillAr
     float ks = 0.f, vs = 0.f;
     const int32_t *pages = p.g.table + (size_t)rt.b * p.g.max_pages;
     const int unfinished = rt.len / kPBT;  // this block is in 16 bits
-    auto fetch = [&](int t) {
+    auto fetch = [&](int t) __attribute__((always_inline)) {
         if (t >= t1 || t == unfinished) return;
         int page = uniform(pages[t]);
         const bool ok = (unsigned)page < (unsigned)p.g.n_pages;
@@ -208,148 +222,61 @@ __global__ __launch_bounds__(kPreThreads, 2) void paged_prefill_kernel(PrefillAr
     };
     fetch(t0);
     // the last key that this wave's rows see, and the first
-    const int wave_last = past + min(rt.place + min(32 * wave + 31, p.per_tile * G - 1) / G, rt.fresh - 1);
-    const bool wave_live = 32 * wave < p.per_tile * G && rt.place + 32 * wave / G < rt.fresh;
-    const int wave_first = past + rt.place + 32 * wave / G;
+    const int wave_last = uniform(past + min(rt.place + min(32 * wave + 31, p.per_tile * G - 1) / G, rt.fresh - 1));
+    const int wave_first = uniform(past + rt.place + 32 * wave / G);
+    const bool wave_live = 32 * wave < p.per_tile * G && wave_first < past + rt.fresh;
 
-    for (int t = t0; t < t1; t++) {
-        uint4 *sk = s_tiles + (t & 1) * 2 * kUnits, *sv = sk + kUnits;
-        float k_scale = ks, v_mant = 1.f;
-        int e;
-        if (t != unfinished) {
-            e = vs > 0.f ? (int)(__float_as_uint(vs) >> 23) - 127 : -127;
-            if (e > -127) v_mant = ldexpf(vs, -e);
-            else if (vs > 0.f) { e = ilogbf(vs); v_mant = ldexpf(vs, -e); }
-            const int top = max(e, e_ref);
-            const float by = e - top < -24 && C == kI8 ? 0.f : ldexpf(1.f, max(e - top, -100));
+    const int token_row = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);  // of K's 32, see above
+    auto rescale = [&](float by) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < kPieces; i++) {
-                const int piece = tid + i * kPreThreads;
-                const int token = piece / (D / 16), chunk = piece % (D / 16) * 2;
-                sk[k_unit<D>(token, chunk)] = widen8_by<C>(ck[i].x, ck[i].y, 1.f);
-                sk[k_unit<D>(token, chunk + 1)] = widen8_by<C>(ck[i].z, ck[i].w, 1.f);
-                const int channel = piece / 4, part = piece % 4 * 2;
-                sv[v_unit(channel, part)] = widen8_by<C>(cv[i].x, cv[i].y, by);
-                sv[v_unit(channel, part + 1)] = widen8_by<C>(cv[i].z, cv[i].w, by);
-            }
-        } else {
-            // the block that is still in 16 bits: K as it is (bf16: times a power of two), V turned and brought to the accumulators' unit
-            const int count = rt.len - unfinished * kPBT;
-            const size_t at = ((size_t)uniform(p.g.tails[rt.b]) * p.g.H + h) * kPBT * D;
-            constexpr int kRowUnits = D / 8, kMine = kUnits / kPreThreads;
-            uint4 wk[kMine], wv[kMine];
-            uint32_t bk = 0, bv = 0;
-#pragma unroll
-            for (int i = 0; i < kMine; i++) {
-                const int u = tid + i * kPreThreads, token = u / kRowUnits;
-                wk[i] = wv[i] = make_uint4(0, 0, 0, 0);
-                if (token < count) {
-                    wk[i] = *reinterpret_cast<const uint4 *>(p.g.k_tail + at + (size_t)u * 8);
-                    wv[i] = *reinterpret_cast<const uint4 *>(p.g.v_tail + at + (size_t)u * 8);
-                }
-            }
-            auto largest = [](uint32_t m, uint32_t w) {
-                const uint32_t lo = w & 0x7fffu, hi = (w >> 16) & 0x7fffu;
-                m = lo < kInfBits<T> && lo > m ? lo : m;
-                return hi < kInfBits<T> && hi > m ? hi : m;
-            };
-#pragma unroll
-            for (int i = 0; i < kMine; i++) {
-                bk = largest(largest(largest(largest(bk, wk[i].x), wk[i].y), wk[i].z), wk[i].w);
-                bv = largest(largest(largest(largest(bv, wv[i].x), wv[i].y), wv[i].z), wv[i].w);
-            }
-            for (int x = 1; x < 64; x <<= 1) {
-                bk = max(bk, (uint32_t)__shfl_xor((int)bk, x));
-                bv = max(bv, (uint32_t)__shfl_xor((int)bv, x));
-            }
-            if (lane == 0) {
-                s_big[0][wave] = bk;
-                s_big[1][wave] = bv;
-            }
-            __syncthreads();
-            for (int i = 0; i < kPreWaves; i++) {
-                bk = max(bk, s_big[0][i]);
-                bv = max(bv, s_big[1][i]);
-            }
-            // the largest V to 2^14 .. 2^15; in fp16 the exponent of subnormal magnitudes counts as the smallest normal one
-            const int shift_k = T == kBF16 ? bf16_shift(bk) : 0;
-            const int shift_v = T == kBF16 ? bf16_shift(bv) : 29 - (int)max(bv >> 10, 1u);
-            k_scale = ldexpf(1.f, -shift_k);
-            e = -shift_v;
-            const int down = e - max(e, e_ref) + shift_v;
-#pragma unroll
-            for (int i = 0; i < kMine; i++) {
-                const int u = tid + i * kPreThreads, token = u / kRowUnits, chunk = u % kRowUnits;
-                uint32_t x[4] = {wk[i].x, wk[i].y, wk[i].z, wk[i].w};
-                if constexpr (T == kBF16) {
-#pragma unroll
-                    for (int c = 0; c < 4; c++) x[c] = bf16_to_half2(x[c], shift_k);
-                }
-                sk[k_unit<D>(token, chunk)] = make_uint4(x[0], x[1], x[2], x[3]);
-                const uint32_t y[4] = {wv[i].x, wv[i].y, wv[i].z, wv[i].w};
-#pragma unroll
-                for (int c = 0; c < 8; c++) {
-                    const float v = c & 1 ? wide_hi<T>(y[c >> 1]) : wide_lo<T>(y[c >> 1]);
-                    reinterpret_cast<_Float16 *>(sv + v_unit(8 * chunk + c, token >> 3))[token & 7] = (_Float16)ldexpf(v, down);
-                }
-            }
-        }
-        fetch(t + 1);
-        __syncthreads();
-        const float by_e = e > e_ref ? ldexpf(1.f, max(e_ref - e, -200)) : 1.f;  // the accumulators to a larger unit
-        e_ref = max(e_ref, e);
-        const bool skip = !wave_live || t * kPBT > wave_last || (p.a.window > 0 && t * kPBT + kPBT - 1 <= wave_first - p.a.window);
-        if (skip) {
-            if (by_e != 1.f) {
-#pragma unroll
-                for (int c = 0; c < D / 32; c++) st.o[c] *= by_e;
-            }
-            continue;
-        }
-
+        for (int c = 0; c < D / 32; c++) st.o[c] *= by;
+    };
+    // Block t, staged: k_scale and mant as above, by_e brings the accumulators to the unit that V was staged in.
+    auto compute = [&](int t, const uint4 *sk, const uint4 *sv, float k_scale, float mant, float by_e, bool masked) __attribute__((always_inline)) {
         float16v s[2];
-        const int token = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
 #pragma unroll
-        for (int j = 0; j < 2; j++) {
+        for (int j = 0; j < 2; j++)
 #pragma unroll
             for (int i = 0; i < 16; i++) s[j][i] = 0.f;
 #pragma unroll
-            for (int k = 0; k < KS; k++)
-                s[j] = mfma32(__builtin_bit_cast(half8v, sk[k_unit<D>(32 * j + token, 2 * k + half)]), qf[k], s[j]);
-        }
+        for (int k = 0; k < KS; k++)
+#pragma unroll
+            for (int j = 0; j < 2; j++)
+                s[j] = mfma32(__builtin_bit_cast(half8v, sk[k_unit<D>(32 * j + token_row, 2 * k + half)]), qf[k], s[j]);
+        ahead<2 * KS>();
         const float f = k_scale * q_factor;
-        const bool masked = t * kPBT + kPBT - 1 > wave_first || (p.a.window > 0 && t * kPBT <= wave_last - p.a.window);
-        const int low = p.a.window > 0 ? pos - p.a.window : -1;
-        auto hidden = [&](int j, int i) {
-            const int key = t * kPBT + 32 * j + 16 * (i >> 3) + 8 * half + (i & 7);
-            return key > pos || key <= low;
-        };
-        float mx = -INFINITY;
+        uint32_t seen[2] = {~0u, ~0u};  // a bit per key of mine
         if (masked) {
+            const int low = p.a.window > 0 ? pos - p.a.window : -1;
 #pragma unroll
             for (int j = 0; j < 2; j++)
 #pragma unroll
-                for (int i = 0; i < 16; i++) mx = fmaxf(mx, hidden(j, i) ? -INFINITY : s[j][i]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 2; j++)
-#pragma unroll
-                for (int i = 0; i < 16; i++) mx = fmaxf(mx, s[j][i]);
+                for (int i = 0; i < 16; i++) {
+                    const int key = t * kPBT + 32 * j + 16 * (i >> 3) + 8 * half + (i & 7);
+                    if (key > pos || key <= low) {
+                        seen[j] &= ~(1u << i);
+                        s[j][i] = -INFINITY;
+                    }
+                }
         }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 2; j++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) mx = fmaxf(mx, s[j][i]);
         {
             const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
             mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * f;
         }
         const bool move = mx - st.ref > kRefMost;
-        if (__builtin_amdgcn_ballot_w64(move) || by_e != 1.f) {
+        if (__builtin_amdgcn_ballot_w64(move) != 0 || by_e != 1.f) {
             const float ref = move ? fmaxf(mx, kLowestRef) - kRefLead : st.ref;
             const float alpha = move ? __builtin_amdgcn_exp2f(st.ref - ref) : 1.f;
             st.ref = ref;
             st.sum *= alpha;
-#pragma unroll
-            for (int c = 0; c < D / 32; c++) st.o[c] *= alpha * by_e;
+            rescale(alpha * by_e);
         }
-        const float mant = __builtin_amdgcn_logf(v_mant), off = mant - st.ref;
+        const float off = mant - st.ref;
         uint32_t pw[2][8];
         float sum = 0.f;
         const half2v ones = {(_Float16)1.f, (_Float16)1.f};
@@ -357,14 +284,20 @@ __global__ __launch_bounds__(kPreThreads, 2) void paged_prefill_kernel(PrefillAr
         for (int j = 0; j < 2; j++)
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
-                float a = __builtin_amdgcn_exp2f(fmaf(s[j][i], f, off)), b = __builtin_amdgcn_exp2f(fmaf(s[j][i + 1], f, off));
-                if (masked) {
-                    a = hidden(j, i) ? 0.f : a;
-                    b = hidden(j, i + 1) ? 0.f : b;
-                }
+                const float a = __builtin_amdgcn_exp2f(fmaf(s[j][i], f, off)), b = __builtin_amdgcn_exp2f(fmaf(s[j][i + 1], f, off));
                 pw[j][i >> 1] = narrow2<kF16>(a, b);
-                sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, pw[j][i >> 1]), ones, sum, false);
             }
+        if (masked) {  // whatever the powers of hidden scores came to (a scale of zero, a reference that nothing has set)
+#pragma unroll
+            for (int j = 0; j < 2; j++)
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    pw[j][i] &= ((seen[j] >> (2 * i)) & 1 ? 0xffffu : 0u) | ((seen[j] >> (2 * i + 1)) & 1 ? 0xffff0000u : 0u);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; j++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, pw[j][i]), ones, sum, false);
         st.sum = fmaf(sum, __builtin_amdgcn_exp2f(-mant), st.sum);
 #pragma unroll
         for (int x = 0; x < 4; x++) {
@@ -373,6 +306,117 @@ __global__ __launch_bounds__(kPreThreads, 2) void paged_prefill_kernel(PrefillAr
 #pragma unroll
             for (int c = 0; c < D / 32; c++)
                 st.o[c] = mfma32(__builtin_bit_cast(half8v, sv[v_unit(32 * c + n, 2 * x + half)]), pf, st.o[c]);
+        }
+        ahead<D / 8>();
+    };
+    // Which of a block's keys this wave's rows see.
+    auto none_seen = [&](int t) {
+        return !wave_live || t * kPBT > wave_last || (p.a.window > 0 && t * kPBT + kPBT - 1 <= wave_first - p.a.window);
+    };
+    auto some_hidden = [&](int t) { return t * kPBT + kPBT - 1 > wave_first || (p.a.window > 0 && t * kPBT <= wave_last - p.a.window); };
+
+    const int t_pages = min(t1, unfinished);
+    auto step = [&](int t, uint4 *sk) __attribute__((always_inline)) {
+        uint4 *sv = sk + kUnits;
+        const float k_scale = __uint_as_float(uniform((int)__float_as_uint(ks)));
+        const float v_scale = __uint_as_float(uniform((int)__float_as_uint(vs)));
+        int e = -127;
+        float mant = 0.f;  // log2 of V's mantissa
+        if (v_scale > 0.f) {
+            e = ilogbf(v_scale);
+            mant = __builtin_amdgcn_logf(ldexpf(v_scale, -e));
+        }
+        const int top = max(e, e_ref);
+        const float by = e - top < -24 && C == kI8 ? 0.f : ldexpf(1.f, max(e - top, -100));
+        const float by_e = e > e_ref ? ldexpf(1.f, max(e_ref - e, -200)) : 1.f;  // the accumulators to a larger unit
+        e_ref = top;
+#pragma unroll
+        for (int i = 0; i < kPieces; i++) {
+            const int piece = tid + i * kPreThreads;
+            const int token = piece / (D / 16), chunk = piece % (D / 16) * 2;
+            sk[k_unit<D>(token, chunk)] = widen8_by<C>(ck[i].x, ck[i].y, 1.f);
+            sk[k_unit<D>(token, chunk + 1)] = widen8_by<C>(ck[i].z, ck[i].w, 1.f);
+            const int channel = piece / 4, part = piece % 4 * 2;
+            sv[v_unit(channel, part)] = widen8_by<C>(cv[i].x, cv[i].y, by);
+            sv[v_unit(channel, part + 1)] = widen8_by<C>(cv[i].z, cv[i].w, by);
+        }
+        fetch(t + 1);
+        __syncthreads();
+        if (none_seen(t)) {
+            if (by_e != 1.f) rescale(by_e);
+        } else {
+            compute(t, sk, sv, k_scale, mant, by_e, some_hidden(t));
+        }
+    };
+    for (int t = t0; t < t_pages; t += 2) {  // the two buffers in turn, their addresses constants
+        step(t, s_tiles);
+        if (t + 1 < t_pages) step(t + 1, s_tiles + 2 * kUnits);
+    }
+    if (t_pages < t1) {
+        // the block that is still in 16 bits: K as it is (bf16: times a power of two), V turned and brought to the accumulators' unit
+        const int t = unfinished, count = rt.len - t * kPBT;
+        uint4 *sk = s_tiles + ((t - t0) & 1) * 2 * kUnits, *sv = sk + kUnits;
+        const size_t at = ((size_t)uniform(p.g.tails[rt.b]) * p.g.H + h) * kPBT * D;
+        constexpr int kRowUnits = D / 8, kMine = kUnits / kPreThreads;
+        uint32_t bk = 0, bv = 0;
+        auto largest = [](uint32_t m, uint4 v) {
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                const uint32_t w = c == 0 ? v.x : c == 1 ? v.y : c == 2 ? v.z : v.w, lo = w & 0x7fffu, hi = (w >> 16) & 0x7fffu;
+                m = lo < kInfBits<T> && lo > m ? lo : m;
+                m = hi < kInfBits<T> && hi > m ? hi : m;
+            }
+            return m;
+        };
+        const uint4 *tk = reinterpret_cast<const uint4 *>(p.g.k_tail + at), *tv = reinterpret_cast<const uint4 *>(p.g.v_tail + at);
+#pragma unroll
+        for (int i = 0; i < kMine; i++) {
+            const int u = tid + i * kPreThreads;
+            if (u / kRowUnits >= count) break;
+            if (T == kBF16) bk = largest(bk, tk[u]);
+            bv = largest(bv, tv[u]);
+        }
+        for (int x = 1; x < 64; x <<= 1) {
+            bk = max(bk, (uint32_t)__shfl_xor((int)bk, x));
+            bv = max(bv, (uint32_t)__shfl_xor((int)bv, x));
+        }
+        if (lane == 0) {
+            s_big[0][wave] = bk;
+            s_big[1][wave] = bv;
+        }
+        __syncthreads();
+        for (int i = 0; i < kPreWaves; i++) {
+            bk = max(bk, s_big[0][i]);
+            bv = max(bv, s_big[1][i]);
+        }
+        // the largest V to 2^14 .. 2^15; in fp16 the exponent of subnormal magnitudes counts as the smallest normal one
+        const int shift_k = T == kBF16 ? bf16_shift(uniform(bk)) : 0;
+        const int shift_v = T == kBF16 ? bf16_shift(uniform(bv)) : 29 - (int)max((uint32_t)uniform(bv) >> 10, 1u);
+        const int e = -shift_v, top = max(e, e_ref);
+        const float by_e = e > e_ref ? ldexpf(1.f, max(e_ref - e, -200)) : 1.f;
+        e_ref = top;
+        for (int u = tid; u < kUnits; u += kPreThreads) {
+            const int row = u / kRowUnits, chunk = u % kRowUnits;
+            uint4 x = make_uint4(0, 0, 0, 0), y = x;
+            if (row < count) {
+                x = tk[u];
+                y = tv[u];
+            }
+            if constexpr (T == kBF16)
+                x = make_uint4(bf16_to_half2(x.x, shift_k), bf16_to_half2(x.y, shift_k), bf16_to_half2(x.z, shift_k), bf16_to_half2(x.w, shift_k));
+            sk[k_unit<D>(row, chunk)] = x;
+            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int c = 0; c < 8; c++) {
+                const float v = c & 1 ? wide_hi<T>(w[c >> 1]) : wide_lo<T>(w[c >> 1]);
+                reinterpret_cast<_Float16 *>(sv + v_unit(8 * chunk + c, row >> 3))[row & 7] = (_Float16)ldexpf(v, -top);
+            }
+        }
+        __syncthreads();
+        if (none_seen(t)) {
+            if (by_e != 1.f) rescale(by_e);
+        } else {
+            compute(t, sk, sv, ldexpf(1.f, -shift_k), 0.f, by_e, true);
         }
     }
 
