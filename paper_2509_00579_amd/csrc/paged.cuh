@@ -61,8 +61,7 @@ constexpr int kMaxDecodeBatch = 4096;
 constexpr int kTicketWords = 1024;
 constexpr int partial_pitch(int D) { return D + 4; }
 
-constexpr int kPrefillSplitWGs = 1024;  // most workgroups of a prefill launch that splits the keys
-constexpr int kPrefillRows = 128;      // query rows of one of them
+constexpr int kPrefillStateRows = 1 << 17;  // rows of states that a prefill launch that splits the keys may leave
 
 hipError_t launch_paged_prefill(const PagedGeo &g, const PagedAttn &a, const int32_t *starts, int n_tokens, int max_new, int max_len,
                                 int head_dim, int data_type, int code_type, hipStream_t s);

@@ -119,7 +119,7 @@ kvcomp_status kvcomp_paged_append(const kvcomp_paged_config *cfg, const kvcomp_p
 
 size_t kvcomp_paged_workspace_bytes(const kvcomp_paged_config *cfg) {
     if (check_config(cfg)) return 0;
-    const size_t decode = (size_t)2 * kDecodeWGs * kDecodeRows, prefill = (size_t)kPrefillSplitWGs * kPrefillRows;  // rows of states
+    const size_t decode = (size_t)2 * kDecodeWGs * kDecodeRows, prefill = kPrefillStateRows;  // rows of states
     return 4 * (kTicketWords + (decode > prefill ? decode : prefill) * partial_pitch(cfg->head_dim));
 }
 

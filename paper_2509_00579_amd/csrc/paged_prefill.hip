@@ -15,6 +15,7 @@
 //
 // Few rows over a long axis: the keys are split among workgroups, and a second launch joins their states.
 #include <algorithm>
+#include <cmath>
 
 #include "huff_decode.cuh"
 #include "paged.cuh"
@@ -24,8 +25,6 @@ namespace kvc {
 
 namespace {
 
-constexpr int kPreWaves = 4, kPreRows = 32 * kPreWaves, kPreThreads = 64 * kPreWaves;
-static_assert(kPreRows == kPrefillRows, "the workspace is laid out for them");
 constexpr float kRefLead = 8.f, kRefMost = 14.f;
 
 struct PrefillArgs {
@@ -38,6 +37,9 @@ struct PrefillArgs {
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ float16v mfma32(half8v a, half8v b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+// How many of the waves' registers a CU has room for, with W waves of 32 rows.
+constexpr int workgroups_per_cu(int D, int W) { return W == 8 ? 1 : D == 128 ? 2 : 3; }
 
 // The row tile of a unit: which sequence, its first token among the sequence's new ones.
 struct RowTile {
@@ -143,9 +145,10 @@ __device__ __forceinline__ void store_rows(uint16_t *out, int half, const RowSta
                 make_uint2(narrow2<T>(st.o[c][i] * f, st.o[c][i + 1] * f), narrow2<T>(st.o[c][i + 2] * f, st.o[c][i + 3] * f));
 }
 
-template <int T, int C, int D>
-__global__ __launch_bounds__(kPreThreads, 2) void paged_prefill_kernel(PrefillArgs p) {
-    constexpr int kUnits = kPBT * D / 8, kPieces = kPBT * D / 16 / kPreThreads;  // 16-byte units of a tile; pieces of 16 codes per thread
+template <int T, int C, int D, int W>
+__global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill_kernel(PrefillArgs p) {
+    constexpr int kPreWaves = W, kPreRows = 32 * W, kPreThreads = 64 * W;
+    constexpr int kUnits = kPBT * D / 8, kPieces = (kPBT * D / 16 + kPreThreads - 1) / kPreThreads;  // 16-byte units of a tile; pieces of 16 codes per thread
     extern __shared__ __align__(16) uint4 s_tiles[];  // [2 buffers][K, V][kUnits]
     __shared__ uint32_t s_big[2][kPreWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n = lane & 31, half = lane >> 5;
@@ -214,9 +217,9 @@ __global__ __launch_bounds__(kPreThreads, 2) void paged_prefill_kernel(PrefillAr
         const size_t tile = (size_t)page * p.g.H + h;
         const uint4 *k = reinterpret_cast<const uint4 *>(p.g.k_codes + tile * kPBT * D), *v = reinterpret_cast<const uint4 *>(p.g.v_codes + tile * kPBT * D);
 #pragma unroll
-        for (int i = 0; i < kPieces; i++) ck[i] = k[tid + i * kPreThreads];
+        for (int i = 0; i < kPieces; i++) if (tid + i * kPreThreads < kPBT * D / 16) ck[i] = k[tid + i * kPreThreads];
 #pragma unroll
-        for (int i = 0; i < kPieces; i++) cv[i] = v[tid + i * kPreThreads];
+        for (int i = 0; i < kPieces; i++) if (tid + i * kPreThreads < kPBT * D / 16) cv[i] = v[tid + i * kPreThreads];
         ks = ok ? p.g.scales[tile * 2] : __builtin_nanf("");
         vs = p.g.scales[tile * 2 + 1];
     };
@@ -333,6 +336,7 @@ __global__ __launch_bounds__(kPreThreads, 2) void paged_prefill_kernel(PrefillAr
 #pragma unroll
         for (int i = 0; i < kPieces; i++) {
             const int piece = tid + i * kPreThreads;
+            if (piece >= kPBT * D / 16) break;
             const int token = piece / (D / 16), chunk = piece % (D / 16) * 2;
             sk[k_unit<D>(token, chunk)] = widen8_by<C>(ck[i].x, ck[i].y, 1.f);
             sk[k_unit<D>(token, chunk + 1)] = widen8_by<C>(ck[i].z, ck[i].w, 1.f);
@@ -449,70 +453,100 @@ __global__ __launch_bounds__(kPreThreads, 2) void paged_prefill_kernel(PrefillAr
     }
 }
 
-// Joins the splits of a row tile: one wave per row, D / 64 channels a lane.
-constexpr int kJoinRows = 16;
+// Joins the splits of a row tile: one wave per row, D / 64 channels a lane.  Lane s has the state of split s, so all weights are
+// known after one load; the accumulators of eight splits are on their way together.
+constexpr int kJoinWaves = 4, kMaxKeySplits = 64;
 template <int T, int D>
-__global__ __launch_bounds__(256) void paged_join_kernel(PrefillArgs p) {
-    constexpr int kJoinGroups = kPreRows / kJoinRows;
+__global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PrefillArgs p, int tile_rows) {
+    constexpr int kMine = D / 64, kBatch = 8;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-    const int group = blockIdx.x % kJoinGroups, rest = blockIdx.x / kJoinGroups, h = rest % p.g.H, unit = rest / p.g.H;
+    const int groups = tile_rows / kJoinWaves, group = uniform(blockIdx.x % groups), rest = uniform(blockIdx.x / groups);
+    const int h = uniform(rest % p.g.H), unit = uniform(rest / p.g.H), r = group * kJoinWaves + wave;
     const RowTile rt = find_tile(p, unit, lane);
     if (rt.b < 0) return;
-    for (int r = group * kJoinRows + wave; r < (group + 1) * kJoinRows; r += 4) {
-        const int place = rt.place + r / p.g.G;
-        if (r >= p.per_tile * p.g.G || place >= rt.fresh) return;
-        const float *part = p.a.partials + ((size_t)(unit * p.g.H + h) * p.splits * kPreRows + r) * partial_pitch(D);
-        const size_t step = (size_t)kPreRows * partial_pitch(D);
-        float top = -INFINITY, e_top = -140.f;
-        for (int s = 0; s < p.splits; s++) {
-            top = fmaxf(top, part[s * step + D]);
-            e_top = fmaxf(e_top, part[s * step + D + 2]);
-        }
-        float sum = 0.f, o[D / 64];
-#pragma unroll
-        for (int c = 0; c < D / 64; c++) o[c] = 0.f;
-        for (int s = 0; s < p.splits; s++) {
-            const float m = part[s * step + D], l = part[s * step + D + 1];
-            const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-            sum += m == -INFINITY ? (l != l ? l : 0.f) : l * f;  // a split that met nothing takes no part
-            const float fo = f * __builtin_amdgcn_exp2f(part[s * step + D + 2] - e_top);
-#pragma unroll
-            for (int c = 0; c < D / 64; c++) o[c] = fmaf(part[s * step + lane * (D / 64) + c], fo, o[c]);
-        }
-        const float f = sum == 0.f ? 0.f : 1.f / sum, unit_v = ldexpf(1.f, (int)e_top);
-        uint16_t *out = p.a.out + (size_t)(rt.start + place) * p.a.out_stride + (size_t)(h * p.g.G + r % p.g.G) * D + lane * (D / 64);
-        if constexpr (D == 128) *reinterpret_cast<uint32_t *>(out) = narrow2<T>(o[0] * f * unit_v, o[1] * f * unit_v);
-        else *out = (uint16_t)narrow2<T>(o[0] * f * unit_v, 0.f);
+    const int place = uniform(rt.place + r / p.g.G);
+    if (r >= p.per_tile * p.g.G || place >= rt.fresh) return;
+    const float *part = p.a.partials + ((size_t)(unit * p.g.H + h) * p.splits * tile_rows + r) * partial_pitch(D);
+    const size_t step = (size_t)tile_rows * partial_pitch(D);
+    float m = -INFINITY, l = 0.f, e = -140.f;
+    if (lane < p.splits) {
+        const float4 s = *reinterpret_cast<const float4 *>(part + lane * step + D);
+        m = s.x;
+        l = s.y;
+        e = s.z;
     }
+    const float top = wave_max(m), e_top = wave_max(e);
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+    const float sum = wave_sum(m == -INFINITY ? (l != l ? l : 0.f) : l * f);  // a split that met nothing takes no part
+    const float w = f * __builtin_amdgcn_exp2f(e - e_top);
+    float o[kMine] = {};
+    for (int s = 0; s < p.splits; s += kBatch) {
+        float v[kBatch][kMine];
+#pragma unroll
+        for (int k = 0; k < kBatch; k++)
+#pragma unroll
+            for (int c = 0; c < kMine; c++) v[k][c] = s + k < p.splits ? part[(s + k) * step + lane * kMine + c] : 0.f;
+#pragma unroll
+        for (int k = 0; k < kBatch; k++)
+#pragma unroll
+            for (int c = 0; c < kMine; c++) o[c] = fmaf(v[k][c], bcast(w, (s + k) & 63), o[c]);
+    }
+    const float by = sum == 0.f ? 0.f : 1.f / sum, unit_v = ldexpf(1.f, (int)e_top);
+    uint16_t *out = p.a.out + (size_t)(rt.start + place) * p.a.out_stride + (size_t)(h * p.g.G + r % p.g.G) * D + lane * kMine;
+    if constexpr (D == 128) *reinterpret_cast<uint32_t *>(out) = narrow2<T>(o[0] * by * unit_v, o[1] * by * unit_v);
+    else *out = (uint16_t)narrow2<T>(o[0] * by * unit_v, 0.f);
 }
 
-template <int T, int C, int D>
-hipError_t launch(PrefillArgs p, int max_len, hipStream_t s) {
+template <int T, int C, int D, int W>
+hipError_t launch_tiles(PrefillArgs p, int max_len, hipStream_t s) {
     constexpr size_t kLds = (size_t)4 * kPBT * D * 2;
-    auto kernel = paged_prefill_kernel<T, C, D>;
+    auto kernel = paged_prefill_kernel<T, C, D, W>;
     static std::atomic<uint64_t> allowed{0};
     hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), kLds, allowed);
     if (e != hipSuccess) return e;
-    p.per_tile = kPreRows / p.g.G;
+    p.per_tile = 32 * W / p.g.G;
     // every sequence has at most one row tile that is not full
-    p.units = p.n_tokens / p.per_tile + (p.g.batch < p.n_tokens ? p.g.batch : p.n_tokens);
-    const long long base = (long long)p.units * p.g.H, pages = max_len > 0 && max_len < p.g.max_pages * kPBT ? (max_len + kPBT - 1) / kPBT : p.g.max_pages;
-    p.splits = (int)std::max(1ll, std::min((long long)kPrefillSplitWGs / base, pages / 8));
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(base * p.splits)), dim3(kPreThreads), kLds, s, p);
+    const int some = p.g.batch < p.n_tokens ? p.g.batch : p.n_tokens;
+    p.units = p.n_tokens / p.per_tile + some;
+    const long long base = (long long)p.units * p.g.H;
+    const int pages = max_len > 0 && max_len < p.g.max_pages * kPBT ? (max_len + kPBT - 1) / kPBT : p.g.max_pages;
+    // Splits of the keys, by what they would take in blocks per workgroup: as many rounds as the workgroups that there are likely
+    // to be need, at least the longest one, and what a split costs by itself (its state's way to memory and back).
+    const double tiles = (double)((p.n_tokens + p.per_tile - 1) / p.per_tile + (some - 1) / 2) * p.g.H;
+    const double longest = p.a.window > 0 ? std::min<double>(pages, (p.a.window + p.per_tile) / kPBT + 2) : pages;
+    const double mean = std::max(longest / 2, longest - (double)p.n_tokens / some / kPBT / 2);
+    const int slots = 256 * workgroups_per_cu(D, W);
+    double best = 0;
+    p.splits = 1;
+    for (int k = 1; k <= kMaxKeySplits && (k == 1 || (k * 4 <= longest && base * k * 32 * W <= kPrefillStateRows)); k++) {
+        const double rounds = std::max(1.0, std::ceil(tiles * k / slots)), extra = k == 1 ? 0 : 3 * rounds + 6 + 0.1 * k;
+        const double cost = std::max(rounds * mean / k, longest / k) + extra;
+        if (k == 1 || cost < best) {
+            best = cost;
+            p.splits = k;
+        }
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(base * p.splits)), dim3(64 * W), kLds, s, p);
     if (p.splits > 1)
-        hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3((unsigned)(base * (kPreRows / kJoinRows))), dim3(256), 0, s, p);
+        hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3((unsigned)(base * (32 * W / kJoinWaves))), dim3(64 * kJoinWaves), 0, s, p, 32 * W);
     return hipGetLastError();
+}
+
+template <int T, int C, int D>
+hipError_t launch(const PrefillArgs &p, int max_new, int max_len, hipStream_t s) {
+    const char *ev = getenv("PW");
+    if (ev ? atoi(ev) == 8 : D == 128) return launch_tiles<T, C, D, 8>(p, max_len, s);
+    return launch_tiles<T, C, D, 4>(p, max_len, s);
 }
 
 }  // namespace
 
 hipError_t launch_paged_prefill(const PagedGeo &g, const PagedAttn &a, const int32_t *starts, int n_tokens, int max_new, int max_len,
                                 int head_dim, int data_type, int code_type, hipStream_t s) {
-    (void)max_new;
     PrefillArgs p = {g, a, n_tokens, 0, 0, 0, starts};
     auto by_dim = [&](auto t, auto c) {
-        if (head_dim == 64) return launch<decltype(t)::value, decltype(c)::value, 64>(p, max_len, s);
-        return launch<decltype(t)::value, decltype(c)::value, 128>(p, max_len, s);
+        if (head_dim == 64) return launch<decltype(t)::value, decltype(c)::value, 64>(p, max_new, max_len, s);
+        return launch<decltype(t)::value, decltype(c)::value, 128>(p, max_new, max_len, s);
     };
     auto by_code = [&](auto t) {
         if (code_type == kI8) return by_dim(t, std::integral_constant<int, kI8>());
