@@ -128,6 +128,13 @@ __device__ __forceinline__ void ahead() {
     __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
 }
 
+// A barrier that waits for LDS only: loads from memory stay on their way.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // What a wave has gathered for its 32 rows; lane (n, half) has row n.
 template <int D>
 struct RowState {
@@ -202,41 +209,26 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
     st.sum = 0.f;
     int e_ref = -10000;  // the accumulators are in units of 2^e_ref
 
-    uint4 ck[kPieces], cv[kPieces];
-    float ks = 0.f, vs = 0.f;
-    const int32_t *pages = p.g.table + (size_t)rt.b * p.g.max_pages;
-    const int unfinished = rt.len / kPBT;  // this block is in 16 bits
-    auto fetch = [&](int t) __attribute__((always_inline)) {
-        if (t >= t1 || t == unfinished) return;
-        int page = uniform(pages[t]);
-        const bool ok = (unsigned)page < (unsigned)p.g.n_pages;
-        if (!ok) {
-            if (tid == 0) flag(p.g.fault, kFaultPage);
-            page = 0;
-        }
-        const size_t tile = (size_t)page * p.g.H + h;
-        const uint4 *k = reinterpret_cast<const uint4 *>(p.g.k_codes + tile * kPBT * D), *v = reinterpret_cast<const uint4 *>(p.g.v_codes + tile * kPBT * D);
-#pragma unroll
-        for (int i = 0; i < kPieces; i++) if (tid + i * kPreThreads < kPBT * D / 16) ck[i] = k[tid + i * kPreThreads];
-#pragma unroll
-        for (int i = 0; i < kPieces; i++) if (tid + i * kPreThreads < kPBT * D / 16) cv[i] = v[tid + i * kPreThreads];
-        ks = ok ? p.g.scales[tile * 2] : __builtin_nanf("");
-        vs = p.g.scales[tile * 2 + 1];
-    };
-    fetch(t0);
-    // the last key that this wave's rows see, and the first
+    const int token_row = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);  // of K's 32, see above
+    // the last key that this wave's rows see, and the first row's
     const int wave_last = uniform(past + min(rt.place + min(32 * wave + 31, p.per_tile * G - 1) / G, rt.fresh - 1));
     const int wave_first = uniform(past + rt.place + 32 * wave / G);
-    const bool wave_live = 32 * wave < p.per_tile * G && wave_first < past + rt.fresh;
+    auto some_hidden = [&](int t) { return t * kPBT + kPBT - 1 > wave_first || (p.a.window > 0 && t * kPBT <= wave_last - p.a.window); };
 
-    const int token_row = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);  // of K's 32, see above
+    float16v s[2];       // scores
+    uint32_t pw[2][8];   // weights, fp16
     auto rescale = [&](float by) __attribute__((always_inline)) {
 #pragma unroll
         for (int c = 0; c < D / 32; c++) st.o[c] *= by;
     };
-    // Block t, staged: k_scale and mant as above, by_e brings the accumulators to the unit that V was staged in.
-    auto compute = [&](int t, const uint4 *sk, const uint4 *sv, float k_scale, float mant, float by_e, bool masked) __attribute__((always_inline)) {
-        float16v s[2];
+    // Where this lane reads K and V of a buffer: the numbers of the 16-byte units within a row differ in bits that the addresses
+    // have to themselves, so each is one exclusive or away from these (which are kept out of the compiler's sight: it
+    // would hold all of them in registers over the loop).
+    const char *tiles = reinterpret_cast<const char *>(s_tiles);
+    const uint32_t k_first = 16 * k_unit<D>(token_row, half), v_first = 16 * v_unit(n, half);
+    auto scores = [&](int buffer) __attribute__((always_inline)) {
+        uint32_t at = k_first + buffer * (2 * kUnits * 16);
+        asm volatile("" : "+v"(at));
 #pragma unroll
         for (int j = 0; j < 2; j++)
 #pragma unroll
@@ -245,8 +237,11 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         for (int k = 0; k < KS; k++)
 #pragma unroll
             for (int j = 0; j < 2; j++)
-                s[j] = mfma32(__builtin_bit_cast(half8v, sk[k_unit<D>(32 * j + token_row, 2 * k + half)]), qf[k], s[j]);
+                s[j] = mfma32(*reinterpret_cast<const half8v *>(tiles + (at ^ (k << 5)) + j * 32 * D * 2), qf[k], s[j]);
         ahead<2 * KS>();
+    };
+    // Scores of block t to weights; mant: log2 of its V scale's mantissa, inv: one over that mantissa, by_e brings the accumulators to the unit that V is staged in.
+    auto weigh = [&](int t, float k_scale, float mant, float inv, float by_e, bool masked) __attribute__((always_inline)) {
         const float f = k_scale * q_factor;
         uint32_t seen[2] = {~0u, ~0u};  // a bit per key of mine
         if (masked) {
@@ -280,7 +275,6 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
             rescale(alpha * by_e);
         }
         const float off = mant - st.ref;
-        uint32_t pw[2][8];
         float sum = 0.f;
         const half2v ones = {(_Float16)1.f, (_Float16)1.f};
 #pragma unroll
@@ -301,65 +295,134 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         for (int j = 0; j < 2; j++)
 #pragma unroll
             for (int i = 0; i < 8; i++) sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, pw[j][i]), ones, sum, false);
-        st.sum = fmaf(sum, __builtin_amdgcn_exp2f(-mant), st.sum);
+        st.sum = fmaf(sum, inv, st.sum);
+    };
+    auto add_values = [&](int buffer) __attribute__((always_inline)) {
+        uint32_t at = v_first + buffer * (2 * kUnits * 16) + kUnits * 16;
+        asm volatile("" : "+v"(at));
 #pragma unroll
         for (int x = 0; x < 4; x++) {
             const uint32_t *w = pw[x >> 1] + 4 * (x & 1);
             const half8v pf = __builtin_bit_cast(half8v, make_uint4(w[0], w[1], w[2], w[3]));
 #pragma unroll
             for (int c = 0; c < D / 32; c++)
-                st.o[c] = mfma32(__builtin_bit_cast(half8v, sv[v_unit(32 * c + n, 2 * x + half)]), pf, st.o[c]);
+                st.o[c] = mfma32(*reinterpret_cast<const half8v *>(tiles + (at ^ (x << 5)) + c * 32 * kPBT * 2), pf, st.o[c]);
         }
         ahead<D / 8>();
     };
-    // Which of a block's keys this wave's rows see.
-    auto none_seen = [&](int t) {
-        return !wave_live || t * kPBT > wave_last || (p.a.window > 0 && t * kPBT + kPBT - 1 <= wave_first - p.a.window);
-    };
-    auto some_hidden = [&](int t) { return t * kPBT + kPBT - 1 > wave_first || (p.a.window > 0 && t * kPBT <= wave_last - p.a.window); };
 
+    // Page numbers and scales of 64 blocks, a block a lane; V's as its exponent, log2 of its mantissa and what takes that out again.
+    const int32_t *pages = p.g.table + (size_t)rt.b * p.g.max_pages;
+    const int unfinished = rt.len / kPBT;  // this block is in 16 bits
     const int t_pages = min(t1, unfinished);
-    auto step = [&](int t, uint4 *sk) __attribute__((always_inline)) {
-        uint4 *sv = sk + kUnits;
-        const float k_scale = __uint_as_float(uniform((int)__float_as_uint(ks)));
-        const float v_scale = __uint_as_float(uniform((int)__float_as_uint(vs)));
-        int e = -127;
-        float mant = 0.f;  // log2 of V's mantissa
-        if (v_scale > 0.f) {
-            e = ilogbf(v_scale);
-            mant = __builtin_amdgcn_logf(ldexpf(v_scale, -e));
+    int known = t0, known_page = 0, known_e = -127;
+    float known_k = 0.f, known_mant = 0.f, known_inv = 1.f;
+    auto learn = [&](int t) __attribute__((always_inline)) {
+        known = t;
+        if (t + lane < t_pages) {
+            known_page = pages[t + lane];
+            const bool ok = (unsigned)known_page < (unsigned)p.g.n_pages;
+            if (!ok) {
+                flag(p.g.fault, kFaultPage);
+                known_page = 0;
+            }
+            const float2 sc = *reinterpret_cast<const float2 *>(p.g.scales + ((size_t)known_page * p.g.H + h) * 2);
+            known_k = ok ? sc.x : __builtin_nanf("");
+            const bool any = sc.y > 0.f;
+            known_e = any ? ilogbf(sc.y) : -127;
+            known_mant = any ? __builtin_amdgcn_logf(ldexpf(sc.y, -known_e)) : 0.f;
+            known_inv = __builtin_amdgcn_exp2f(-known_mant);
         }
-        const int top = max(e, e_ref);
-        const float by = e - top < -24 && C == kI8 ? 0.f : ldexpf(1.f, max(e - top, -100));
-        const float by_e = e > e_ref ? ldexpf(1.f, max(e_ref - e, -200)) : 1.f;  // the accumulators to a larger unit
-        e_ref = top;
+    };
+    auto e_of = [&](int t) { return __builtin_amdgcn_readlane(known_e, t - known); };
+    auto power_of_2 = [&](int e) { return __uint_as_float((uint32_t)max(e + 127, 0) << 23); };  // 0 below the normal range
+    auto to_larger = [&](int e) { return power_of_2(min(e_ref - e, 0)); };
+
+    // Two halves of the workgroup's waves, one of each on every SIMD, take turns: while one multiplies (block t's weights with V,
+    // then its queries with block t + 1's K), the other weighs its scores and widens its share of the codes of a later block.
+    constexpr int kGroups = W == 8 ? 2 : 1;
+    const int lead = kGroups == 2 ? wave >> 2 : 0;
+    constexpr int kTilePieces = kPBT * D / 16;
+    const int k_piece = tid, v_piece = kTilePieces < kPreThreads ? (tid + kPreThreads / 2) % kPreThreads : tid;
+    uint4 ck[kPieces], cv[kPieces];
+    int e_staged = -10000;
+    // Behind the last block the same is done with it again, into buffers that nobody will read: a branch around it would cost the
+    // loop copies of whatever it leaves in registers.
+    auto fetch_k = [&](int t) __attribute__((always_inline)) {
+        t = min(t, t_pages - 1);
+        const uint4 *k = reinterpret_cast<const uint4 *>(p.g.k_codes + ((size_t)__builtin_amdgcn_readlane(known_page, t - known) * p.g.H + h) * kPBT * D);
+#pragma unroll
+        for (int i = 0; i < kPieces; i++)
+            if (k_piece + i * kPreThreads < kTilePieces) ck[i] = k[k_piece + i * kPreThreads];
+    };
+    auto fetch_v = [&](int t) __attribute__((always_inline)) {
+        t = min(t, t_pages - 1);
+        const uint4 *v = reinterpret_cast<const uint4 *>(p.g.v_codes + ((size_t)__builtin_amdgcn_readlane(known_page, t - known) * p.g.H + h) * kPBT * D);
+#pragma unroll
+        for (int i = 0; i < kPieces; i++)
+            if (v_piece + i * kPreThreads < kTilePieces) cv[i] = v[v_piece + i * kPreThreads];
+    };
+    auto stage_k = [&](uint4 *sk) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < kPieces; i++) {
-            const int piece = tid + i * kPreThreads;
-            if (piece >= kPBT * D / 16) break;
-            const int token = piece / (D / 16), chunk = piece % (D / 16) * 2;
+            const int piece = k_piece + i * kPreThreads, token = piece / (D / 16), chunk = piece % (D / 16) * 2;
+            if (piece >= kTilePieces) break;
             sk[k_unit<D>(token, chunk)] = widen8_by<C>(ck[i].x, ck[i].y, 1.f);
             sk[k_unit<D>(token, chunk + 1)] = widen8_by<C>(ck[i].z, ck[i].w, 1.f);
-            const int channel = piece / 4, part = piece % 4 * 2;
+        }
+    };
+    auto stage_v = [&](int t, uint4 *sv) __attribute__((always_inline)) {
+        const int e = e_of(min(t, t_pages - 1));
+        e_staged = max(e, e_staged);
+        const float by = e - e_staged < (C == kI8 ? -24 : -100) ? 0.f : power_of_2(e - e_staged);
+#pragma unroll
+        for (int i = 0; i < kPieces; i++) {
+            const int piece = v_piece + i * kPreThreads, channel = piece / 4, part = piece % 4 * 2;
+            if (piece >= kTilePieces) break;
             sv[v_unit(channel, part)] = widen8_by<C>(cv[i].x, cv[i].y, by);
             sv[v_unit(channel, part + 1)] = widen8_by<C>(cv[i].z, cv[i].w, by);
         }
-        fetch(t + 1);
-        __syncthreads();
-        if (none_seen(t)) {
-            if (by_e != 1.f) rescale(by_e);
-        } else {
-            compute(t, sk, sv, k_scale, mant, by_e, some_hidden(t));
-        }
     };
-    for (int t = t0; t < t_pages; t += 2) {  // the two buffers in turn, their addresses constants
-        step(t, s_tiles);
-        if (t + 1 < t_pages) step(t + 1, s_tiles + 2 * kUnits);
+    if (t0 < t_pages) {
+        auto buffer = [&](int t) { return s_tiles + ((t - t0) & 1) * 2 * kUnits; };
+        learn(t0);
+        fetch_k(t0);
+        stage_k(s_tiles);
+        if (lead) {
+            fetch_k(t0 + 1);
+            fetch_v(t0);
+            stage_k(s_tiles + 2 * kUnits);
+            stage_v(t0, s_tiles + kUnits);
+        }
+        fetch_k(t0 + 1 + lead);
+        fetch_v(t0 + lead);
+        lds_barrier();
+        scores(0);
+        if (lead) lds_barrier();
+        for (int t = t0; t < t_pages; t++) {
+            if (t + 4 > known + 64) learn(t);
+            const int mine = (t - t0) & 1;
+            const int e = e_of(t);
+            const float by_e = to_larger(e);
+            e_ref = max(e, e_ref);
+            weigh(t, bcast(known_k, t - known), bcast(known_mant, t - known), bcast(known_inv, t - known), by_e, some_hidden(t));
+            stage_k(buffer(t + 1 + lead));
+            stage_v(t + lead, buffer(t + lead) + kUnits);
+            fetch_k(t + 2 + lead);
+            fetch_v(t + 1 + lead);
+            lds_barrier();
+            __builtin_amdgcn_s_setprio(1);
+            add_values(mine);
+            scores(1 - mine);
+            __builtin_amdgcn_s_setprio(0);
+            if (kGroups == 2) lds_barrier();
+        }
+        if (kGroups == 2 && !lead) lds_barrier();
     }
     if (t_pages < t1) {
         // the block that is still in 16 bits: K as it is (bf16: times a power of two), V turned and brought to the accumulators' unit
         const int t = unfinished, count = rt.len - t * kPBT;
-        uint4 *sk = s_tiles + ((t - t0) & 1) * 2 * kUnits, *sv = sk + kUnits;
+        uint4 *sk = s_tiles, *sv = sk + kUnits;
         const size_t at = ((size_t)uniform(p.g.tails[rt.b]) * p.g.H + h) * kPBT * D;
         constexpr int kRowUnits = D / 8, kMine = kUnits / kPreThreads;
         uint32_t bk = 0, bv = 0;
@@ -397,7 +460,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         const int shift_k = T == kBF16 ? bf16_shift(uniform(bk)) : 0;
         const int shift_v = T == kBF16 ? bf16_shift(uniform(bv)) : 29 - (int)max((uint32_t)uniform(bv) >> 10, 1u);
         const int e = -shift_v, top = max(e, e_ref);
-        const float by_e = e > e_ref ? ldexpf(1.f, max(e_ref - e, -200)) : 1.f;
+        const float by_e = to_larger(e);
         e_ref = top;
         for (int u = tid; u < kUnits; u += kPreThreads) {
             const int row = u / kRowUnits, chunk = u % kRowUnits;
@@ -417,11 +480,9 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
             }
         }
         __syncthreads();
-        if (none_seen(t)) {
-            if (by_e != 1.f) rescale(by_e);
-        } else {
-            compute(t, sk, sv, ldexpf(1.f, -shift_k), 0.f, by_e, true);
-        }
+        scores(0);
+        weigh(t, ldexpf(1.f, -shift_k), 0.f, 1.f, by_e, true);
+        add_values(0);
     }
 
     float sum;
@@ -534,8 +595,7 @@ hipError_t launch_tiles(PrefillArgs p, int max_len, hipStream_t s) {
 
 template <int T, int C, int D>
 hipError_t launch(const PrefillArgs &p, int max_new, int max_len, hipStream_t s) {
-    const char *ev = getenv("PW");
-    if (ev ? atoi(ev) == 8 : D == 128) return launch_tiles<T, C, D, 8>(p, max_len, s);
+    if (D == 128 && (max_new == 0 || (long long)max_new * p.g.G > 128)) return launch_tiles<T, C, D, 8>(p, max_len, s);
     return launch_tiles<T, C, D, 4>(p, max_len, s);
 }
 
