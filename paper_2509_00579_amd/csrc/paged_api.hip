@@ -155,7 +155,7 @@ kvcomp_status kvcomp_paged_attn_decode(const kvcomp_paged_config *cfg, const kvc
     if (q_len < 1 || q_len > kDecodeRows || q_len * g.G > kDecodeRows)
         return fail(KVCOMP_ERR_INVALID_ARG, "q_len must be at least 1, and q_len times the group of query heads at most %d", kDecodeRows);
     if (g.batch > kMaxDecodeBatch) return fail(KVCOMP_ERR_INVALID_ARG, "more than %d sequences", kMaxDecodeBatch);
-    if ((long long)g.batch * g.H * g.max_pages > 0x7fffffffll)
+    if ((long long)g.batch * g.H * (g.max_pages + 8) > 0x7fffffffll)
         return fail(KVCOMP_ERR_INVALID_ARG, "more than 2^31 - 1 sequences times KV heads times max_pages");
     if (max_len < 0) return fail(KVCOMP_ERR_INVALID_ARG, "max_len is negative");
     if (!g.batch) return KVCOMP_OK;

@@ -34,6 +34,14 @@ __device__ __forceinline__ half8v as_half8(uint32_t x, uint32_t y, uint32_t z, u
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 constexpr float kRefBelow = 15.f;
+#ifndef TU
+#define TU 3
+#endif
+#ifndef LU
+#define LU 1
+#endif
+constexpr int kTailUnits = TU;   // what an unfinished block costs, in pages
+constexpr int kLeastUnits = LU;  // units of work per wave that another workgroup is worth
 // bf16: the accumulators hold 2^-40 of the sums, so that neither the largest values overflow them (2^15 of a weight, 2^26 keys)
 // nor the largest weight's of anything that a page holds (2^-100 and more) drops below binary32's normal range; the factor
 // is a multiplication of its own, since with it the smallest scales would.
@@ -171,65 +179,62 @@ struct Wave {
         }
     }
 
-    // Tiles [i0, i1) of a head whose first tile is `first`.
-    __device__ __forceinline__ void run(int b, int h, int first, int i0, int i1, int len) {
-        const int whole = min(i1, len / kPBT - first);  // those that are pages
+    // Pages [i0, whole) of a head whose first tile is `first`.
+    __device__ __forceinline__ void run(int b, int h, int first, int i0, int whole, int len) {
+        if (i0 >= whole) return;
         const int32_t *pages = p.g.table + (size_t)b * p.g.max_pages + first;
-        if (i0 < whole) {
-            int page, next = 0;
-            float ks, vs, ks_next = 0.f, vs_next = 0.f;
-            auto scales = [&](int &pg, float &k, float &v) {
-                const bool ok = (unsigned)pg < (unsigned)p.g.n_pages;
+        // page numbers and scales of 64 tiles, a tile a lane
+        int known = i0, known_page = 0;
+        float known_k = 0.f, known_v = 0.f;
+        auto learn = [&](int i) {
+            known = i;
+            if (i + lane < whole) {
+                known_page = pages[i + lane];
+                const bool ok = (unsigned)known_page < (unsigned)p.g.n_pages;
                 if (!ok) {
-                    if (lane == 0) flag(p.g.fault, kFaultPage);
-                    pg = 0;
+                    flag(p.g.fault, kFaultPage);
+                    known_page = 0;
                 }
-                const float *sc = p.g.scales + ((size_t)pg * p.g.H + h) * 2;
-                k = ok ? sc[0] : kNan;
-                v = sc[1];
-            };
-            page = uniform(pages[i0]);
-            if (i0 + 1 < whole) next = uniform(pages[i0 + 1]);
-            scales(page, ks, vs);
-            load_k(page, h);
-            load_v(page, h);
-            for (int i = i0; i < whole; i++) {
-                float4v s[R][4];
+                const float2 sc = *reinterpret_cast<const float2 *>(p.g.scales + ((size_t)known_page * p.g.H + h) * 2);
+                known_k = ok ? sc.x : kNan;
+                known_v = sc.y;
+            }
+        };
+        auto page_at = [&](int i) { return __builtin_amdgcn_readlane(known_page, i - known); };
+        learn(i0);
+        load_k(page_at(i0), h);
+        load_v(page_at(i0), h);
+        for (int i = i0; i < whole; i++) {
+            float4v s[R][4];
 #pragma unroll
-                for (int t = 0; t < 4; t++) {
+            for (int t = 0; t < 4; t++) {
 #pragma unroll
-                    for (int r = 0; r < R; r++) s[r][t] = float4v{0.f, 0.f, 0.f, 0.f};
+                for (int r = 0; r < R; r++) s[r][t] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int j = 0; j < KJ; j++) {
-                        const half8v k0 = widen8<C>(kr[t][j].x, kr[t][j].y), k1 = widen8<C>(kr[t][j].z, kr[t][j].w);
+                for (int j = 0; j < KJ; j++) {
+                    const half8v k0 = widen8<C>(kr[t][j].x, kr[t][j].y), k1 = widen8<C>(kr[t][j].z, kr[t][j].w);
 #pragma unroll
-                        for (int r = 0; r < R; r++) {
-                            s[r][t] = mfma16(k0, qf[r][2 * j], s[r][t]);
-                            s[r][t] = mfma16(k1, qf[r][2 * j + 1], s[r][t]);
-                        }
+                    for (int r = 0; r < R; r++) {
+                        s[r][t] = mfma16(k0, qf[r][2 * j], s[r][t]);
+                        s[r][t] = mfma16(k1, qf[r][2 * j + 1], s[r][t]);
                     }
                 }
-                const bool more = i + 1 < whole;
-                if (more) {
-                    scales(next, ks_next, vs_next);
-                    load_k(next, h);
-                }
-                float x[R][16], alpha[R];
-                half8v hi[R][2], lo[R][2];
-                scores(s, ks * p.a.scale, (first + i) * kPBT, len, x);
-                softmax(x, hi, lo, alpha);
-#pragma unroll
-                for (int c = 0; c < CT; c++)
-                    add_v(c, widen8<C>(vr[c].x, vr[c].y), widen8<C>(vr[c].z, vr[c].w), hi, lo, alpha, vs);
-                if (more) {
-                    load_v(next, h);
-                    ks = ks_next;
-                    vs = vs_next;
-                    if (i + 2 < whole) next = uniform(pages[i + 2]);
-                }
             }
+            const float ks = bcast(known_k, i - known), vs = bcast(known_v, i - known);
+            const bool more = i + 1 < whole;
+            if (more) {
+                if (i + 1 == known + 64) learn(i + 1);
+                load_k(page_at(i + 1), h);
+            }
+            float x[R][16], alpha[R];
+            half8v hi[R][2], lo[R][2];
+            scores(s, ks * p.a.scale, (first + i) * kPBT, len, x);
+            softmax(x, hi, lo, alpha);
+#pragma unroll
+            for (int c = 0; c < CT; c++)
+                add_v(c, widen8<C>(vr[c].x, vr[c].y), widen8<C>(vr[c].z, vr[c].w), hi, lo, alpha, vs);
+            if (more) load_v(page_at(i + 1), h);
         }
-        if (whole < i1) unfinished(b, h, len);
     }
 
     // The block that is still in 16 bits: K as it is, V turned in registers, rows behind the end left out.
@@ -370,48 +375,48 @@ template <int T, int C, int D, int R>
 __global__ __launch_bounds__(64 * decode_waves(R)) void paged_decode_kernel(DecodeArgs p) {
     constexpr int kWaves = decode_waves(R), kThreads = 64 * kWaves, kSlots = 2 * kWaves, kPitch = partial_pitch(D), kQuads = D / 4;
     extern __shared__ __align__(16) float s_dyn[];
-    __shared__ int s_b[kSlots], s_h[kSlots];
-    __shared__ uint32_t s_total, s_last[2];
+    __shared__ int4 s_of[kSlots];  // whose state is parked: sequence (-1: none), head, the head's first unit and how many have an owner
+    __shared__ uint32_t s_last[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int slot_floats = p.rows * kPitch;
     uint32_t *before = reinterpret_cast<uint32_t *>(s_dyn + max(kSlots * slot_floats, kThreads * 4 + 2 * kDecodeWGs * p.rows));  // tiles of one head of the sequences before
 
-    auto sane = [&](int b, int len) {
-        return (unsigned)len <= (unsigned)p.g.max_pages * kPBT && (len % kPBT == 0 || (unsigned)p.g.tails[b] < (unsigned)p.g.n_tails);
+    // Units of work of one head of a sequence: a page is one, an unfinished block `kTailUnits` (none: an empty place, or one that
+    // does not fit).  Every wave takes the sums for itself and leaves the same words in LDS, so nobody waits.
+    auto sane = [&](int len, int tail) {
+        return (unsigned)len <= (unsigned)p.g.max_pages * kPBT && (len % kPBT == 0 || (unsigned)tail < (unsigned)p.g.n_tails);
     };
-    auto count_of = [&](int b) -> uint32_t {
-        const int len = p.g.lens[b];
-        return sane(b, len) && len > 0 ? (uint32_t)tiles_of(len, p.q_len, p.a.window).count : 0u;
-    };
-    if (wave == 0) {
-        uint32_t sum = 0;
-        for (int base = 0; base < p.g.batch; base += 64) {
-            const uint32_t mine = base + lane < p.g.batch ? count_of(base + lane) : 0u;
-            const uint32_t ex = wave_excl_scan(mine, lane);
-            if (base + lane < p.g.batch) before[base + lane] = sum + ex;
-            sum += __builtin_amdgcn_readlane(ex + mine, 63);
+    auto pages_of = [&](int len) { return len / kPBT - tiles_of(len, p.q_len, p.a.window).first; };
+    uint32_t sum = 0;
+    int first_lens = 0;  // of the first 64 sequences
+    for (int base = 0; base < p.g.batch; base += 64) {
+        uint32_t mine = 0;
+        if (base + lane < p.g.batch) {
+            const int len = p.g.lens[base + lane], tail = p.g.tails[base + lane];
+            if (base == 0) first_lens = len;
+            if (sane(len, tail) && len > 0) mine = pages_of(len) + (len % kPBT ? kTailUnits : 0);
         }
-        if (lane == 0) {
-            before[p.g.batch] = sum;
-            s_total = sum;
-        }
+        const uint32_t ex = wave_excl_scan(mine, lane);
+        if (base + lane < p.g.batch) before[base + lane] = sum + ex;
+        sum += __builtin_amdgcn_readlane(ex + mine, 63);
     }
-    if (lane < 2) s_b[2 * wave + lane] = -1;
-    __syncthreads();
+    if (lane == 0) before[p.g.batch] = sum;
+    if (lane < 2) s_of[2 * wave + lane].x = -1;
+    wave_sync();
     // empty places: zeros; those that do not fit: NaN
     for (int b = blockIdx.x; b < p.g.batch; b += gridDim.x) {
         if (before[b + 1] != before[b]) continue;
         const int len = p.g.lens[b];
-        const bool ok = sane(b, len);
+        const bool ok = sane(len, p.g.tails[b]);
         if (!ok && tid == 0) flag(p.g.fault, (unsigned)len <= (unsigned)p.g.max_pages * kPBT ? kFaultTail : kFaultLength);
         const uint32_t w = ok ? 0u : kNanBits<T> * 0x10001u;
         const int per_row = p.g.H * p.g.G * D / 8;
         for (int i = tid; i < p.q_len * per_row; i += kThreads)
             *reinterpret_cast<uint4 *>(p.a.out + ((size_t)b * p.q_len + i / per_row) * p.a.out_stride + (size_t)(i % per_row) * 8) = make_uint4(w, w, w, w);
     }
-    const uint32_t H = p.g.H, total = s_total * H;
-    // no more workgroups than there are tiles for their waves
-    const uint32_t active = min((uint32_t)gridDim.x, (total + kWaves - 1) / kWaves), wg = blockIdx.x;
+    const uint32_t H = p.g.H, total = sum * H;
+    // no more workgroups than there is work for their waves
+    const uint32_t active = min((uint32_t)gridDim.x, (total + kWaves * kLeastUnits - 1) / (kWaves * kLeastUnits)), wg = blockIdx.x;
     if (wg >= active) return;
     const Deal deal(total, active);
     const uint32_t wg_begin = deal.begin(wg), wg_end = deal.begin(wg + 1);
@@ -436,48 +441,55 @@ __global__ __launch_bounds__(64 * decode_waves(R)) void paged_decode_kernel(Deco
             continue;
         }
         const uint32_t in_seq = t - base * H, h = in_seq / tiles, i0 = in_seq - h * tiles, i1 = min(tiles, i0 + (t_end - t));
-        const int len = uniform(p.g.lens[b]);
+        const int len = b < 64 ? __builtin_amdgcn_readlane(first_lens, b) : uniform(p.g.lens[b]);
+        t += i1 - i0;
+        const uint32_t pages = pages_of(len), tail = len % kPBT ? 1 : 0;
+        if (i0 >= pages + tail) continue;  // the rest of an unfinished block's units: it belongs to the first one's owner
         w.begin(b, (int)h);
-        w.run(b, (int)h, tiles_of(len, p.q_len, p.a.window).first, (int)i0, (int)i1, len);
-        if (i1 - i0 == tiles) {
+        w.run(b, (int)h, tiles_of(len, p.q_len, p.a.window).first, (int)min(i0, pages), (int)min(i1, pages), len);
+        if (tail && i0 <= pages && pages < i1) w.unfinished(b, (int)h, len);
+        if (i0 == 0 && i1 >= pages + tail) {
             w.store(b, (int)h);
         } else {
             w.park(s_dyn + (size_t)(2 * wave + parked) * slot_floats);
-            if (lane == 0) {
-                s_b[2 * wave + parked] = b;
-                s_h[2 * wave + parked] = (int)h;
-            }
+            if (lane == 0) s_of[2 * wave + parked] = make_int4(b, (int)h, (int)(base * H + h * tiles), (int)(pages + tail));
             parked++;
         }
-        t += i1 - i0;
     }
     __syncthreads();
 
     // Join the parked states of each head; a head that other workgroups have a part of leaves its state in the workspace.
     int open = 0, open_b[2], open_h[2];
-    for (int s0 = 0; s0 < kSlots;) {
-        const int sb = uniform(s_b[s0]), sh = uniform(s_h[s0]);
-        if (sb < 0) {
-            s0++;
-            continue;
-        }
-        int s1 = s0 + 1;
-        while (s1 < kSlots && (uniform(s_b[s1]) < 0 || (uniform(s_b[s1]) == sb && uniform(s_h[s1]) == sh))) s1++;
-        const uint32_t base = before[sb], tiles = before[sb + 1] - base;
-        const uint32_t begin = uniform((int)(base * H + sh * tiles)), end = begin + uniform((int)tiles);
-        const bool complete = begin >= wg_begin && end <= wg_end;
+    uint32_t open_begin[2], open_units[2];
+    const int4 of = s_of[lane & (kSlots - 1)];  // a slot a lane
+    uint32_t left = (uint32_t)__builtin_amdgcn_ballot_w64(of.x >= 0 && lane < kSlots);
+    while (left) {
+        const int s0 = __builtin_ctz(left);
+        const int sb = __builtin_amdgcn_readlane(of.x, s0), sh = __builtin_amdgcn_readlane(of.y, s0);
+        const uint32_t begin = __builtin_amdgcn_readlane(of.z, s0), units = __builtin_amdgcn_readlane(of.w, s0);
+        const uint32_t mine = (uint32_t)__builtin_amdgcn_ballot_w64(of.x == sb && of.y == sh && lane < kSlots);
+        left &= ~mine;
+        const bool complete = begin >= wg_begin && begin + units <= wg_end;
         for (int item = tid; item < p.rows * kQuads; item += kThreads) {
             const int row = item / kQuads, c = (item - row * kQuads) * 4;
-            float top = -INFINITY;
-            for (int s = s0; s < s1; s++)
-                if (s_b[s] >= 0) top = fmaxf(top, s_dyn[s * slot_floats + row * kPitch + D]);
+            const float *at = s_dyn + row * kPitch;
+            float m[kSlots], l[kSlots];
+#pragma unroll
+            for (int s = 0; s < kSlots; s++) {
+                const bool have = (mine >> s) & 1;
+                m[s] = have ? at[s * slot_floats + D] : -INFINITY;
+                l[s] = have ? at[s * slot_floats + D + 1] : 0.f;
+            }
+            float top = kLowestRef;
+#pragma unroll
+            for (int s = 0; s < kSlots; s++) top = fmaxf(top, m[s]);
             float sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-            for (int s = s0; s < s1; s++) {
-                if (s_b[s] < 0) continue;
-                const float *at = s_dyn + s * slot_floats + row * kPitch;
-                const float f = __builtin_amdgcn_exp2f(at[D] - top);
-                const float4 v = *reinterpret_cast<const float4 *>(at + c);
-                sum = fmaf(at[D + 1], f, sum);
+#pragma unroll
+            for (int s = 0; s < kSlots; s++) {
+                if (!((mine >> s) & 1)) continue;
+                const float f = __builtin_amdgcn_exp2f(m[s] - top);
+                const float4 v = *reinterpret_cast<const float4 *>(at + s * slot_floats + c);
+                sum = fmaf(l[s], f, sum);
                 acc[0] = fmaf(v.x, f, acc[0]);
                 acc[1] = fmaf(v.y, f, acc[1]);
                 acc[2] = fmaf(v.z, f, acc[2]);
@@ -486,21 +498,22 @@ __global__ __launch_bounds__(64 * decode_waves(R)) void paged_decode_kernel(Deco
             if (complete) {
                 store_row4<T, D>(p, sb, sh, row, c, acc, sum);
             } else {
-                float *at = p.a.partials + ((size_t)(2 * wg + (begin < wg_begin ? 0 : 1)) * p.rows + row) * kPitch;
+                float *to = p.a.partials + ((size_t)(2 * wg + (begin < wg_begin ? 0 : 1)) * p.rows + row) * kPitch;
 #pragma unroll
-                for (int k = 0; k < 4; k++) store_agent(at + c + k, acc[k]);
+                for (int k = 0; k < 4; k++) store_agent(to + c + k, acc[k]);
                 if (c == 0) {
-                    store_agent(at + D, top);
-                    store_agent(at + D + 1, sum);
+                    store_agent(to + D, top);
+                    store_agent(to + D + 1, sum);
                 }
             }
         }
         if (!complete) {
-            open_b[open & 1] = sb;
-            open_h[open & 1] = sh;
-            open++;
+            const int k = open++ & 1;  // two at most: the one that began before, the one that goes on behind
+            open_b[k] = sb;
+            open_h[k] = sh;
+            open_begin[k] = begin;
+            open_units[k] = units;
         }
-        s0 = s1;
     }
     if (!open) return;
     // every wave: its partial stores have completed before the barrier is passed
@@ -508,8 +521,7 @@ __global__ __launch_bounds__(64 * decode_waves(R)) void paged_decode_kernel(Deco
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     for (int k = 0; k < open; k++) {
-        const uint32_t base = before[open_b[k]], tiles = before[open_b[k] + 1] - base, begin = base * H + open_h[k] * tiles;
-        const uint32_t from = deal.owner(begin), parts = deal.owner(begin + tiles - 1) - from + 1;
+        const uint32_t from = deal.owner(open_begin[k]), parts = deal.owner(open_begin[k] + open_units[k] - 1) - from + 1;
         if (tid == 0) {
             const uint32_t ticket = __hip_atomic_fetch_add(p.a.tickets + from, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             s_last[k] = ticket == parts - 1;
@@ -573,9 +585,9 @@ hipError_t launch(const DecodeArgs &p, int max_len, hipStream_t s) {
     hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), kDecodeLdsBytes, allowed);
     if (e != hipSuccess) return e;
     if (lds > kDecodeLdsBytes) return hipErrorInvalidValue;
-    // tiles there could be: no more workgroups than they can give each wave one
+    // units of work that there could be: no more workgroups than they can busy
     const int pages = max_len > 0 && max_len < p.g.max_pages * kPBT ? (max_len + kPBT - 1) / kPBT : p.g.max_pages;
-    const size_t most = (size_t)p.g.batch * p.g.H * pages, wgs = (most + decode_waves(R) - 1) / decode_waves(R);
+    const size_t most = (size_t)p.g.batch * p.g.H * (pages + kTailUnits), per_wg = decode_waves(R) * kLeastUnits, wgs = (most + per_wg - 1) / per_wg;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(wgs < (size_t)kDecodeWGs ? wgs : (size_t)kDecodeWGs)), dim3(kThreads), lds, s, p);
     return hipGetLastError();
 }

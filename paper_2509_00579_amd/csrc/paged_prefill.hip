@@ -39,7 +39,7 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 __device__ __forceinline__ float16v mfma32(half8v a, half8v b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
 // How many of the waves' registers a CU has room for, with W waves of 32 rows.
-constexpr int workgroups_per_cu(int D, int W) { return W == 8 ? 1 : D == 128 ? 2 : 3; }
+constexpr int workgroups_per_cu(int D, int W) { return W == 8 ? 1 : D == 128 ? 2 : 4; }
 
 // The row tile of a unit: which sequence, its first token among the sequence's new ones.
 struct RowTile {
