@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import pathlib
+import struct
 
 import numpy as np
 import torch
@@ -37,31 +38,18 @@ class Stats(C.Structure):
         return {n: getattr(self, n) for n, _ in self._fields_}
 
 
-class PagedConfig(C.Structure):
-    _fields_ = [(n, C.c_int32) for n in ("n_kv_heads", "n_q_heads", "head_dim", "data_type", "code_type", "n_pages", "n_tails",
-                                         "max_pages")]
-
-
-class PagedTensors(C.Structure):
-    _fields_ = [(n, C.c_void_p) for n in ("d_k_codes", "d_v_codes", "d_scales", "d_k_tail", "d_v_tail", "d_fault")]
-
-
-class PagedBatch(C.Structure):
-    _fields_ = [("batch", C.c_int32), ("d_lens", C.c_void_p), ("d_table", C.c_void_p), ("d_tails", C.c_void_p)]
-
-
-class PagedNew(C.Structure):
-    _fields_ = [("n_tokens", C.c_int32), ("d_starts", C.c_void_p), ("d_k", C.c_void_p), ("d_v", C.c_void_p),
-                ("k_stride", C.c_size_t), ("v_stride", C.c_size_t), ("d_q", C.c_void_p), ("d_q_out", C.c_void_p),
-                ("q_stride", C.c_size_t), ("q_out_stride", C.c_size_t), ("d_cos_sin", C.c_void_p), ("n_positions", C.c_int32),
-                ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32), ("sections", C.c_int32 * 3),
-                ("d_positions", C.c_void_p)]
+# The paged cache's structures as packed bytes (native sizes and alignment): cheaper to make anew for every call than ctypes
+# structures, and a call's arguments stay its own when several threads call.
+_PAGED_CONFIG = struct.Struct("@8i")          # n_kv_heads n_q_heads head_dim data_type code_type n_pages n_tails max_pages
+_PAGED_CACHE = struct.Struct("@6P")           # k_codes v_codes scales k_tail v_tail fault
+_PAGED_BATCH = struct.Struct("@i3P")          # batch lens table tails
+_PAGED_NEW = struct.Struct("@i3P2N2P2NP4i3iP")  # n_tokens starts k v k_stride v_stride q q_out q_stride q_out_stride cos_sin
+#                                               n_positions rot_dim interleaved n_axes sections positions
 
 
 # every symbol include/kvcomp.h declares: name -> (restype, argtypes)
 _vp, _i, _f = C.c_void_p, C.c_int, C.c_float
 _cfgp = C.POINTER(Config)
-_pcfg, _pmem, _pseq, _pnew = C.POINTER(PagedConfig), C.POINTER(PagedTensors), C.POINTER(PagedBatch), C.POINTER(PagedNew)
 SIGNATURES = {
     "kvcomp_arena_bytes": (C.c_size_t, [_cfgp]),
     "kvcomp_create": (_i, [_cfgp, _vp, C.c_size_t, _vp, C.POINTER(_vp)]),
@@ -90,12 +78,12 @@ SIGNATURES = {
     "kvcomp_baseline_workspace_bytes": (C.c_size_t, [_cfgp]),
     "kvcomp_baseline_fp16_attn": (_i, [_cfgp, _vp, _vp, _i, _vp, _f, _vp, _vp, C.c_size_t, _i, _vp]),
     "kvcomp_baseline_fp16_attn_noalloc": (_i, [_cfgp, _vp, _vp, _i, _vp, _f, _vp, _i, _vp]),
-    "kvcomp_paged_append": (_i, [_pcfg, _pmem, _pseq, _pnew, _vp]),
-    "kvcomp_paged_workspace_bytes": (C.c_size_t, [_pcfg]),
-    "kvcomp_paged_attn_decode": (_i, [_pcfg, _pmem, _pseq, _vp, C.c_size_t, _i, _f, _i, _i, _vp, C.c_size_t, _vp, C.c_size_t, _vp]),
-    "kvcomp_paged_attn_prefill": (_i, [_pcfg, _pmem, _pseq, _vp, C.c_size_t, _vp, _i, _f, _i, _i, _i, _vp, C.c_size_t, _vp,
+    "kvcomp_paged_append": (_i, [_vp, _vp, _vp, _vp, _vp]),
+    "kvcomp_paged_workspace_bytes": (C.c_size_t, [_vp]),
+    "kvcomp_paged_attn_decode": (_i, [_vp, _vp, _vp, _vp, C.c_size_t, _i, _f, _i, _i, _vp, C.c_size_t, _vp, C.c_size_t, _vp]),
+    "kvcomp_paged_attn_prefill": (_i, [_vp, _vp, _vp, _vp, C.c_size_t, _vp, _i, _f, _i, _i, _i, _vp, C.c_size_t, _vp,
                                        C.c_size_t, _vp]),
-    "kvcomp_paged_check": (_i, [_pmem, _vp]),
+    "kvcomp_paged_check": (_i, [_vp, _vp]),
     "kvcomp_last_error": (C.c_char_p, []),
 }
 
@@ -390,7 +378,7 @@ class Rope:
         sections = [self.rot_dim // 2] if sections is None else list(sections)
         assert 1 <= len(sections) <= 3, "one to three axes"
         self.interleaved, self.n_axes = int(interleaved), len(sections)
-        self.sections = (C.c_int32 * 3)(*sections)
+        self.sections = tuple(sections) + (0,) * (3 - len(sections))
 
     @staticmethod
     def table(n_positions, rot_dim, base=10000.0, device="cuda:0"):
@@ -429,37 +417,43 @@ class PagedCache:
             setattr(self, name, x)
         self.fault = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._types = (head_dim, {torch.float16: 0, torch.bfloat16: 1}[dtype], int(codes == "e4m3"), n_pages, n_tails)
-        self._memory = PagedTensors(*(x.data_ptr() for x in (*storage, self.fault)))
+        self._memory = _PAGED_CACHE.pack(*(x.data_ptr() for x in (*storage, self.fault)))
+        self._index = self.device.index
         self._config = {}
         self._workspace = None
 
     def _cfg(self, max_pages):
         cfg = self._config.get(max_pages)
         if cfg is None:
-            cfg = self._config[max_pages] = PagedConfig(self.H, self.Hq, *self._types, max_pages)
+            cfg = self._config[max_pages] = _PAGED_CONFIG.pack(self.H, self.Hq, *self._types, max_pages)
         return cfg
 
     def _batch(self, lens, table, tails):
-        i32, dev = torch.int32, self.device
-        n = lens.shape[0]
+        i32, dev, n = torch.int32, self._index, lens.shape[0]
         assert lens.dtype is i32 and table.dtype is i32 and tails.dtype is i32, "lens, table and tails are int32"
-        assert lens.device == dev and table.device == dev and tails.device == dev, f"lens, table and tails must be on {dev}"
-        assert table.dim() == 2 and table.shape[0] == n and tails.shape == (n,) and lens.dim() == 1, "one row per sequence"
+        assert lens.get_device() == dev and table.get_device() == dev and tails.get_device() == dev, (
+            f"lens, table and tails must be on {self.device}")
+        assert lens.dim() == 1 and table.dim() == 2 and table.shape[0] == n and tails.dim() == 1 and tails.shape[0] == n, "one row per sequence"
         assert table.is_contiguous() and lens.is_contiguous() and tails.is_contiguous(), "lens, table and tails must be contiguous"
-        return PagedBatch(n, lens.data_ptr(), table.data_ptr(), tails.data_ptr())
+        return _PAGED_BATCH.pack(n, lens.data_ptr(), table.data_ptr(), tails.data_ptr())
+
+    def _starts(self, starts, batch):
+        assert starts.dtype is torch.int32 and starts.get_device() == self._index and starts.is_contiguous()
+        assert starts.dim() == 1 and starts.shape[0] == batch + 1, "starts: one entry per sequence and the end"
+        return starts.data_ptr()
 
     def _rows(self, x, n, heads, name):
         """Pointer and token stride of a tensor [n, heads, head_dim] whose tokens may be apart (a slice of a fused projection)."""
-        assert x.device == self.device and x.dtype is self.dtype, f"{name} must be {self.dtype} on {self.device}"
+        assert x.get_device() == self._index and x.dtype is self.dtype, f"{name} must be {self.dtype} on {self.device}"
         assert x.shape == (n, heads, self.D), f"{name}: expected shape {(n, heads, self.D)}, got {tuple(x.shape)}"
-        s = x.stride()
-        assert s[2] == 1 and (s[1] == self.D or heads == 1), f"the heads of a token of {name} must be contiguous"
-        return x.data_ptr(), s[0] if n > 1 else heads * self.D
+        s0, s1, s2 = x.stride()
+        assert s2 == 1 and (s1 == self.D or heads == 1), f"the heads of a token of {name} must be contiguous"
+        return x.data_ptr(), s0 if n > 1 else heads * self.D
 
     def _on_device(self):
-        if torch._C._cuda_getDevice() != self.device.index:
+        if torch._C._cuda_getDevice() != self._index:
             raise KvcompError(ERR_INVALID_ARG, f"the current device is not the cache's ({self.device})")
-        return torch._C._cuda_getCurrentRawStream(self.device.index)
+        return torch._C._cuda_getCurrentRawStream(self._index)
 
     def append(self, k, v, lens, table, tails, starts=None, q=None, q_out=None, rope=None, positions=None):
         """Append k, v [n, n_kv_heads, head_dim]: one token per sequence (starts None: n = batch), or rows starts[b] ..
@@ -472,26 +466,26 @@ class PagedCache:
         kp, ks = self._rows(k, n, self.H, "k")
         vp, vs = self._rows(v, n, self.H, "v")
         sp = qp = qs = op = os_ = cp = n_pos = rot = inter = pp = 0
-        axes, sections = 1, (C.c_int32 * 3)()
+        axes, sections = 1, (0, 0, 0)
         if starts is not None:
-            assert starts.dtype is torch.int32 and starts.device == self.device and starts.is_contiguous()
-            assert starts.shape == (lens.shape[0] + 1,), "starts: one entry per sequence and the end"
-            sp = starts.data_ptr()
+            sp = self._starts(starts, lens.shape[0])
         if q is not None:
             if q_out is None:
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
             qp, qs = self._rows(q, n, self.Hq, "q")
             op, os_ = self._rows(q_out, n, self.Hq, "q_out")
         if rope is not None:
-            assert rope.cos_sin.device == self.device
+            assert rope.cos_sin.get_device() == self._index
             cp, n_pos, rot, inter, axes, sections = (rope.cos_sin.data_ptr(), rope.n_positions, rope.rot_dim, rope.interleaved,
                                                      rope.n_axes, rope.sections)
             if positions is not None:
-                assert positions.dtype is torch.int32 and positions.device == self.device and positions.is_contiguous()
+                assert positions.dtype is torch.int32 and positions.get_device() == self._index and positions.is_contiguous()
                 assert positions.shape == (axes, n), f"positions: expected shape {(axes, n)}, got {tuple(positions.shape)}"
                 pp = positions.data_ptr()
-        new = PagedNew(n, sp, kp, vp, ks, vs, qp, op, qs, os_, cp, n_pos, rot, inter, axes, sections, pp)
-        _check(self.lib.kvcomp_paged_append(self._cfg(table.shape[1]), self._memory, seqs, new, stream))
+        new = _PAGED_NEW.pack(n, sp, kp, vp, ks, vs, qp, op, qs, os_, cp, n_pos, rot, inter, axes, *sections, pp)
+        st = self.lib.kvcomp_paged_append(self._cfg(table.shape[1]), self._memory, seqs, new, stream)
+        if st:
+            _check(st)
         return q_out
 
     def new_workspace(self):
@@ -503,7 +497,7 @@ class PagedCache:
             if self._workspace is None:
                 self._workspace = self.new_workspace()
             return self._workspace
-        assert workspace.device == self.device and workspace.dtype is torch.uint8 and workspace.is_contiguous()
+        assert workspace.get_device() == self._index and workspace.dtype is torch.uint8 and workspace.is_contiguous()
         return workspace
 
     def attn_decode(self, q, scale, lens, table, tails, q_len=1, window=0, max_len=0, out=None, workspace=None):
@@ -526,15 +520,14 @@ class PagedCache:
         (starts: int32 [batch + 1]); max_new, max_len: the longest chunk and length, if known."""
         stream = self._on_device()
         seqs = self._batch(lens, table, tails)
-        assert starts.dtype is torch.int32 and starts.device == self.device and starts.is_contiguous()
-        assert starts.shape == (lens.shape[0] + 1,), "starts: one entry per sequence and the end"
+        sp = self._starts(starts, lens.shape[0])
         n = q.shape[0]
         if out is None:
             out = torch.empty((n, self.Hq, self.D), dtype=self.dtype, device=self.device)
         qp, qs = self._rows(q, n, self.Hq, "q")
         op, os_ = self._rows(out, n, self.Hq, "out")
         ws = self._scratch(workspace)
-        _check(self.lib.kvcomp_paged_attn_prefill(self._cfg(table.shape[1]), self._memory, seqs, qp, qs, starts.data_ptr(), n,
+        _check(self.lib.kvcomp_paged_attn_prefill(self._cfg(table.shape[1]), self._memory, seqs, qp, qs, sp, n,
                                                   float(scale), window, max_new, max_len, op, os_, ws.data_ptr(), ws.numel(), stream))
         return out
 

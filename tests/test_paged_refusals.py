@@ -7,6 +7,27 @@ import pytest
 ALIGNED = 1 << 20
 
 
+class Config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_kv_heads", "n_q_heads", "head_dim", "data_type", "code_type", "n_pages", "n_tails",
+                                         "max_pages")]
+
+
+class Tensors(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("d_k_codes", "d_v_codes", "d_scales", "d_k_tail", "d_v_tail", "d_fault")]
+
+
+class Batch(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("d_lens", C.c_void_p), ("d_table", C.c_void_p), ("d_tails", C.c_void_p)]
+
+
+class New(C.Structure):
+    _fields_ = [("n_tokens", C.c_int32), ("d_starts", C.c_void_p), ("d_k", C.c_void_p), ("d_v", C.c_void_p),
+                ("k_stride", C.c_size_t), ("v_stride", C.c_size_t), ("d_q", C.c_void_p), ("d_q_out", C.c_void_p),
+                ("q_stride", C.c_size_t), ("q_out_stride", C.c_size_t), ("d_cos_sin", C.c_void_p), ("n_positions", C.c_int32),
+                ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32), ("sections", C.c_int32 * 3),
+                ("d_positions", C.c_void_p)]
+
+
 @pytest.fixture(scope="module")
 def B():
     from paper_2509_00579_amd import binding, build
@@ -19,19 +40,19 @@ def B():
 def _config(B, **kw):
     d = dict(n_kv_heads=8, n_q_heads=32, head_dim=128, data_type=0, code_type=0, n_pages=100, n_tails=4, max_pages=16)
     d.update(kw)
-    return B.PagedConfig(**d)
+    return C.byref(Config(**d))
 
 
 def _memory(B, **kw):
     d = dict.fromkeys(("d_k_codes", "d_v_codes", "d_scales", "d_k_tail", "d_v_tail", "d_fault"), ALIGNED)
     d.update(kw)
-    return B.PagedTensors(**d)
+    return C.byref(Tensors(**d))
 
 
 def _batch(B, **kw):
     d = dict(batch=3, d_lens=ALIGNED, d_table=ALIGNED, d_tails=ALIGNED)
     d.update(kw)
-    return B.PagedBatch(**d)
+    return C.byref(Batch(**d))
 
 
 def _new(B, **kw):
@@ -39,7 +60,7 @@ def _new(B, **kw):
              q_out_stride=0, d_cos_sin=0, n_positions=0, rot_dim=0, interleaved=0, n_axes=1, sections=(C.c_int32 * 3)(), d_positions=0)
     d.update(kw)
     d["sections"] = (C.c_int32 * 3)(*d["sections"])
-    return B.PagedNew(**d)
+    return C.byref(New(**d))
 
 
 BAD_CONFIGS = [dict(n_kv_heads=0), dict(n_q_heads=33), dict(n_q_heads=0), dict(n_kv_heads=1, n_q_heads=33), dict(head_dim=96),
@@ -167,3 +188,16 @@ def test_nothing_to_attend_is_fine(B):
     assert lib.kvcomp_paged_attn_decode(_config(B), _memory(B), none, *_decode_args(B, q=0, out=0)) == B.OK
     assert lib.kvcomp_paged_attn_prefill(_config(B), _memory(B), none, *_prefill_args(B)) == B.OK
     assert lib.kvcomp_paged_attn_prefill(_config(B), _memory(B), _batch(B), *_prefill_args(B, n_tokens=0, q=0)) == B.OK
+
+
+def test_the_binding_packs_the_structures_of_the_header(B):
+    """Sizes and places of the fields, against ctypes' own layout of the same declarations."""
+    for packer, kind in ((B._PAGED_CONFIG, Config), (B._PAGED_CACHE, Tensors), (B._PAGED_BATCH, Batch), (B._PAGED_NEW, New)):
+        assert packer.size == C.sizeof(kind)
+        n = sum(3 if name == "sections" else 1 for name, _ in kind._fields_)
+        got = kind.from_buffer_copy(packer.pack(*range(1, n + 1)))
+        values = []
+        for name, _ in kind._fields_:
+            v = getattr(got, name)
+            values += list(v) if name == "sections" else [v]
+        assert values == list(range(1, n + 1))
