@@ -31,6 +31,17 @@ __device__ __forceinline__ float4v mfma16(half8v a, half8v b, float4v c) { retur
 __device__ __forceinline__ half8v as_half8(uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
     return __builtin_bit_cast(half8v, make_uint4(x, y, z, w));
 }
+// The same with 16-bit values of type T as they are in memory.
+template <int T>
+__device__ __forceinline__ float4v product(uint4 a, uint4 b, float4v c) {
+    typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+    if constexpr (T == kBF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+    else return mfma16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c);
+}
+__device__ __forceinline__ uint4 half8_to_bf16(half8v v) {
+    return make_uint4(narrow2<kBF16>((float)v[0], (float)v[1]), narrow2<kBF16>((float)v[2], (float)v[3]),
+                      narrow2<kBF16>((float)v[4], (float)v[5]), narrow2<kBF16>((float)v[6], (float)v[7]));
+}
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 constexpr float kRefBelow = 15.f;
@@ -136,27 +147,36 @@ struct Wave {
         }
     }
 
-    // x becomes P as fp16 parts; returns what the state so far is to be multiplied with.
+    // The scores of row group r become weights; returns what the state so far is to be multiplied with.
+    __device__ __forceinline__ float weigh(int r, float (&x)[16]) {
+        float mx = x[0];
+#pragma unroll
+        for (int j = 1; j < 16; j++) mx = fmaxf(mx, x[j]);
+        mx = fmaxf(fmaxf(m[r], max_rows(mx) - kRefBelow), kLowestRef);
+        const float alpha = __builtin_amdgcn_exp2f(m[r] - mx);
+        m[r] = mx;
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 16; j++) {
+            x[j] = __builtin_amdgcn_exp2f(x[j] - mx);
+            sum += x[j];
+        }
+        l[r] = l[r] * alpha + sum;
+        return alpha;
+    }
+    // ... and those P as two fp16 parts.
     __device__ __forceinline__ void softmax(float (&x)[R][16], half8v (&hi)[R][2], half8v (&lo)[R][2], float (&alpha)[R]) {
 #pragma unroll
         for (int r = 0; r < R; r++) {
-            float mx = x[r][0];
-#pragma unroll
-            for (int j = 1; j < 16; j++) mx = fmaxf(mx, x[r][j]);
-            mx = fmaxf(fmaxf(m[r], max_rows(mx) - kRefBelow), kLowestRef);
-            alpha[r] = __builtin_amdgcn_exp2f(m[r] - mx);
-            m[r] = mx;
-            float sum = 0.f;
+            alpha[r] = weigh(r, x[r]);
             uint32_t ph[8], pl[8];
 #pragma unroll
             for (int j = 0; j < 16; j += 2) {
-                const float a = __builtin_amdgcn_exp2f(x[r][j] - mx), b = __builtin_amdgcn_exp2f(x[r][j + 1] - mx);
-                sum += a + b;
+                const float a = x[r][j], b = x[r][j + 1];
                 const auto h = __builtin_amdgcn_cvt_pkrtz(a, b);
                 ph[j >> 1] = __builtin_bit_cast(uint32_t, h);
                 pl[j >> 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a - (float)h[0], b - (float)h[1]));
             }
-            l[r] = l[r] * alpha[r] + sum;
 #pragma unroll
             for (int k = 0; k < 2; k++) {
                 hi[r][k] = as_half8(ph[4 * k], ph[4 * k + 1], ph[4 * k + 2], ph[4 * k + 3]);
@@ -260,51 +280,38 @@ struct Wave {
                 vt[j][0] = w.x; vt[j][1] = w.y;
             }
         }
-        float k_factor = 1.f, v_factor = 1.f;
-        if constexpr (T == kBF16) {
-            uint32_t mk = 0, mv = 0;
-#pragma unroll
-            for (int s = 0; s < 4; s++)
-#pragma unroll
-                for (int x = 0; x < KS; x++)
-                    mk = bf16_largest(bf16_largest(bf16_largest(bf16_largest(mk, kt[s][x].x), kt[s][x].y), kt[s][x].z), kt[s][x].w);
-#pragma unroll
-            for (int j = 0; j < 16; j++)
-#pragma unroll
-                for (int w = 0; w < CT / 2; w++) mv = bf16_largest(mv, vt[j][w]);
-            mk = max_rows_u(mk);
-            mv = max_rows_u(mv);
-            mk = max(mk, dpp_u<kDppXor1>(mk)); mv = max(mv, dpp_u<kDppXor1>(mv));
-            mk = max(mk, dpp_u<kDppXor2>(mk)); mv = max(mv, dpp_u<kDppXor2>(mv));
-            mk = max(mk, dpp_u<kDppHalfMirror>(mk)); mv = max(mv, dpp_u<kDppHalfMirror>(mv));
-            mk = max(mk, dpp_u<kDppMirror>(mk)); mv = max(mv, dpp_u<kDppMirror>(mv));
-            const int sk = bf16_shift(mk), sv = bf16_shift(mv);
-            k_factor = ldexpf(1.f, -sk);
-            v_factor = ldexpf(1.f, -sv);
-#pragma unroll
-            for (int s = 0; s < 4; s++)
-#pragma unroll
-                for (int x = 0; x < KS; x++)
-                    kt[s][x] = make_uint4(bf16_to_half2(kt[s][x].x, sk), bf16_to_half2(kt[s][x].y, sk), bf16_to_half2(kt[s][x].z, sk),
-                                          bf16_to_half2(kt[s][x].w, sk));
-#pragma unroll
-            for (int j = 0; j < 16; j++)
-#pragma unroll
-                for (int w = 0; w < CT / 2; w++) vt[j][w] = bf16_to_half2(vt[j][w], sv);
-        }
         float4v s[R][4];
 #pragma unroll
-        for (int t = 0; t < 4; t++)
+        for (int r = 0; r < R; r++) {
+            uint4 qt[KS];  // bf16 queries are exact in both types
 #pragma unroll
-            for (int r = 0; r < R; r++) {
+            for (int x = 0; x < KS; x++) qt[x] = T == kBF16 ? half8_to_bf16(qf[r][x]) : __builtin_bit_cast(uint4, qf[r][x]);
+#pragma unroll
+            for (int t = 0; t < 4; t++) {
                 s[r][t] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int x = 0; x < KS; x++) s[r][t] = mfma16(__builtin_bit_cast(half8v, kt[t][x]), qf[r][x], s[r][t]);
+                for (int x = 0; x < KS; x++) s[r][t] = product<T>(kt[t][x], qt[x], s[r][t]);
             }
+        }
         float x[R][16], alpha[R];
-        half8v hi[R][2], lo[R][2];
-        scores(s, k_factor * p.a.scale, len - count, len, x);
-        softmax(x, hi, lo, alpha);
+        constexpr int kParts = T == kBF16 ? 3 : 2;  // of 8 and of 11 bits
+        uint32_t parts[R][kParts][8];
+        scores(s, p.a.scale, len - count, len, x);
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            alpha[r] = weigh(r, x[r]);
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+                float a = x[r][j], c = x[r][j + 1];
+#pragma unroll
+                for (int k = 0; k < kParts; k++) {
+                    const uint32_t w = narrow2<T>(a, c);
+                    parts[r][k][j >> 1] = w;
+                    a -= wide_lo<T>(w);
+                    c -= wide_hi<T>(w);
+                }
+            }
+        }
 #pragma unroll
         for (int j = 0; j < 16; j++)
 #pragma unroll
@@ -315,7 +322,18 @@ struct Wave {
 #pragma unroll
             for (int k = 0; k < 8; k++)
                 a[k] = __builtin_amdgcn_perm(vt[2 * k + 1][c >> 1], vt[2 * k][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
-            add_v(c, as_half8(a[0], a[1], a[2], a[3]), as_half8(a[4], a[5], a[6], a[7]), hi, lo, alpha, v_factor);
+#pragma unroll
+            for (int r = 0; r < R; r++) {
+                float4v acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < kParts; k++)
+#pragma unroll
+                    for (int h8 = 0; h8 < 2; h8++)
+                        acc = product<T>(make_uint4(a[4 * h8], a[4 * h8 + 1], a[4 * h8 + 2], a[4 * h8 + 3]),
+                                         make_uint4(parts[r][k][4 * h8], parts[r][k][4 * h8 + 1], parts[r][k][4 * h8 + 2], parts[r][k][4 * h8 + 3]), acc);
+#pragma unroll
+                for (int k = 0; k < 4; k++) o[r][c][k] = fmaf(acc[k], kVUnit<T>, o[r][c][k] * alpha[r]);
+            }
         }
     }
 
@@ -359,9 +377,16 @@ struct Wave {
     }
 };
 
+__device__ __forceinline__ void store_agent2(float *p, float a, float b) {
+    __hip_atomic_store(reinterpret_cast<unsigned long long *>(p), (unsigned long long)__float_as_uint(b) << 32 | __float_as_uint(a),
+                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 load_agent2(const float *p) {
+    const unsigned long long w = __hip_atomic_load(reinterpret_cast<const unsigned long long *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
+}
+
 constexpr size_t kDecodeLdsBytes = 159 * 1024;  // what the kernels may have apart from their own few words
-// Waves of a workgroup: the parked states of two segments per wave have to fit the LDS.
-constexpr int decode_waves(int R) { return R == 1 ? 8 : 4; }
 
 template <int T, int D>
 __device__ __forceinline__ void store_row4(const DecodeArgs &p, int b, int h, int row, int c, const float (&o)[4], float sum) {
@@ -371,15 +396,15 @@ __device__ __forceinline__ void store_row4(const DecodeArgs &p, int b, int h, in
     *reinterpret_cast<uint2 *>(out) = make_uint2(narrow2<T>(o[0] * f, o[1] * f), narrow2<T>(o[2] * f, o[3] * f));
 }
 
-template <int T, int C, int D, int R>
-__global__ __launch_bounds__(64 * decode_waves(R)) void paged_decode_kernel(DecodeArgs p) {
-    constexpr int kWaves = decode_waves(R), kThreads = 64 * kWaves, kSlots = 2 * kWaves, kPitch = partial_pitch(D), kQuads = D / 4;
+template <int T, int C, int D, int R, int W>
+__global__ __launch_bounds__(64 * W) void paged_decode_kernel(DecodeArgs p) {
+    constexpr int kWaves = W, kThreads = 64 * kWaves, kSlots = 2 * kWaves, kPitch = partial_pitch(D), kQuads = D / 4;
     extern __shared__ __align__(16) float s_dyn[];
     __shared__ int4 s_of[kSlots];  // whose state is parked: sequence (-1: none), head, the head's first unit and how many have an owner
     __shared__ uint32_t s_last[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int slot_floats = p.rows * kPitch;
-    uint32_t *before = reinterpret_cast<uint32_t *>(s_dyn + max(kSlots * slot_floats, kThreads * 4 + 2 * kDecodeWGs * p.rows));  // tiles of one head of the sequences before
+    uint32_t *before = reinterpret_cast<uint32_t *>(s_dyn + max(kSlots * slot_floats, kThreads * 6));  // units of one head of the sequences before
 
     // Units of work of one head of a sequence: a page is one, an unfinished block `kTailUnits` (none: an empty place, or one that
     // does not fit).  Every wave takes the sums for itself and leaves the same words in LDS, so nobody waits.
@@ -387,25 +412,28 @@ __global__ __launch_bounds__(64 * decode_waves(R)) void paged_decode_kernel(Deco
         return (unsigned)len <= (unsigned)p.g.max_pages * kPBT && (len % kPBT == 0 || (unsigned)tail < (unsigned)p.g.n_tails);
     };
     auto pages_of = [&](int len) { return len / kPBT - tiles_of(len, p.q_len, p.a.window).first; };
-    uint32_t sum = 0;
-    int first_lens = 0;  // of the first 64 sequences
+    const bool few = p.g.batch <= 64;  // then a sequence is a lane, and nothing goes through LDS
+    uint32_t sum = 0, lane_units = 0, lane_before = 0;
+    int lane_len = 0;
     for (int base = 0; base < p.g.batch; base += 64) {
-        uint32_t mine = 0;
+        lane_units = 0;
         if (base + lane < p.g.batch) {
             const int len = p.g.lens[base + lane], tail = p.g.tails[base + lane];
-            if (base == 0) first_lens = len;
-            if (sane(len, tail) && len > 0) mine = pages_of(len) + (len % kPBT ? kTailUnits : 0);
+            if (sane(len, tail) && len > 0) lane_units = pages_of(len) + (len % kPBT ? kTailUnits : 0);
+            lane_len = len;
         }
-        const uint32_t ex = wave_excl_scan(mine, lane);
-        if (base + lane < p.g.batch) before[base + lane] = sum + ex;
-        sum += __builtin_amdgcn_readlane(ex + mine, 63);
+        lane_before = wave_excl_scan(lane_units, lane);
+        if (!few && base + lane < p.g.batch) before[base + lane] = sum + lane_before;
+        sum += __builtin_amdgcn_readlane(lane_before + lane_units, 63);
     }
-    if (lane == 0) before[p.g.batch] = sum;
+    if (!few && lane == 0) before[p.g.batch] = sum;
     if (lane < 2) s_of[2 * wave + lane].x = -1;
     wave_sync();
+    auto before_of = [&](int b) { return (uint32_t)(few ? __builtin_amdgcn_readlane((int)lane_before, b) : uniform((int)before[b])); };
+    auto units_of = [&](int b) { return (uint32_t)(few ? __builtin_amdgcn_readlane((int)lane_units, b) : uniform((int)(before[b + 1] - before[b]))); };
     // empty places: zeros; those that do not fit: NaN
     for (int b = blockIdx.x; b < p.g.batch; b += gridDim.x) {
-        if (before[b + 1] != before[b]) continue;
+        if (units_of(b) != 0) continue;
         const int len = p.g.lens[b];
         const bool ok = sane(len, p.g.tails[b]);
         if (!ok && tid == 0) flag(p.g.fault, (unsigned)len <= (unsigned)p.g.max_pages * kPBT ? kFaultTail : kFaultLength);
@@ -426,22 +454,26 @@ __global__ __launch_bounds__(64 * decode_waves(R)) void paged_decode_kernel(Deco
 
     Wave<T, C, D, R> w(p, lane);
     int b = 0, parked = 0;
-    if (t < t_end) {  // the sequence of the first tile
-        int lo = 0, hi = p.g.batch;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if ((uint32_t)uniform((int)before[mid]) * H <= t) lo = mid; else hi = mid;
+    if (t < t_end) {  // the sequence of the first unit
+        if (few) {
+            b = __builtin_ctzll(__builtin_amdgcn_ballot_w64((lane_before + lane_units) * H > t));
+        } else {
+            int lo = 0, hi = p.g.batch;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (before_of(mid) * H <= t) lo = mid; else hi = mid;
+            }
+            b = lo;
         }
-        b = lo;
     }
     while (t < t_end) {
-        uint32_t base = (uint32_t)uniform((int)before[b]), tiles = (uint32_t)uniform((int)before[b + 1]) - base;
+        const uint32_t base = before_of(b), tiles = units_of(b);
         if ((base + tiles) * H <= t) {
             b++;
             continue;
         }
         const uint32_t in_seq = t - base * H, h = in_seq / tiles, i0 = in_seq - h * tiles, i1 = min(tiles, i0 + (t_end - t));
-        const int len = b < 64 ? __builtin_amdgcn_readlane(first_lens, b) : uniform(p.g.lens[b]);
+        const int len = few ? __builtin_amdgcn_readlane(lane_len, b) : uniform(p.g.lens[b]);
         t += i1 - i0;
         const uint32_t pages = pages_of(len), tail = len % kPBT ? 1 : 0;
         if (i0 >= pages + tail) continue;  // the rest of an unfinished block's units: it belongs to the first one's owner
@@ -461,7 +493,7 @@ __global__ __launch_bounds__(64 * decode_waves(R)) void paged_decode_kernel(Deco
     // Join the parked states of each head; a head that other workgroups have a part of leaves its state in the workspace.
     int open = 0, open_b[2], open_h[2];
     uint32_t open_begin[2], open_units[2];
-    const int4 of = s_of[lane & (kSlots - 1)];  // a slot a lane
+    const int4 of = s_of[min(lane, kSlots - 1)];  // a slot a lane
     uint32_t left = (uint32_t)__builtin_amdgcn_ballot_w64(of.x >= 0 && lane < kSlots);
     while (left) {
         const int s0 = __builtin_ctz(left);
@@ -499,12 +531,9 @@ __global__ __launch_bounds__(64 * decode_waves(R)) void paged_decode_kernel(Deco
                 store_row4<T, D>(p, sb, sh, row, c, acc, sum);
             } else {
                 float *to = p.a.partials + ((size_t)(2 * wg + (begin < wg_begin ? 0 : 1)) * p.rows + row) * kPitch;
-#pragma unroll
-                for (int k = 0; k < 4; k++) store_agent(to + c + k, acc[k]);
-                if (c == 0) {
-                    store_agent(to + D, top);
-                    store_agent(to + D + 1, sum);
-                }
+                store_agent2(to + c, acc[0], acc[1]);
+                store_agent2(to + c + 2, acc[2], acc[3]);
+                if (c == 0) store_agent2(to + D, top, sum);
             }
         }
         if (!complete) {
@@ -528,68 +557,83 @@ __global__ __launch_bounds__(64 * decode_waves(R)) void paged_decode_kernel(Deco
         }
         __syncthreads();
         if (!s_last[k]) continue;
-        // the last to arrive: all parts' maxima and sums to LDS, then groups of threads take parts in turn
-        float *s_m = s_dyn + kThreads * 4, *s_l = s_m + (size_t)kDecodeWGs * p.rows;
-        auto part_at = [&](uint32_t i) { return p.a.partials + ((size_t)(2 * (from + i) + (i == 0 ? 1 : 0)) * p.rows) * kPitch; };
-        for (uint32_t i = tid; i < parts * p.rows; i += kThreads) {
-            const uint32_t part = i / p.rows, row = i - part * p.rows;
-            s_m[i] = load_agent(part_at(part) + row * kPitch + D);
-            s_l[i] = load_agent(part_at(part) + row * kPitch + D + 1);
-        }
-        __syncthreads();
+        // The last to arrive: groups of threads take the parts in turn, everything that a thread needs of four parts on its way at
+        // once; the groups meet in LDS.
         const int items = p.rows * kQuads, groups = max(1, min(kThreads / items, (int)parts));
-        for (int at = 0; at < items; at += kThreads) {
+        for (int at = 0; at < items; at += kThreads) {  // one round, unless there are more items than threads
             const int local = groups > 1 ? tid % items : tid, group = groups > 1 ? tid / items : 0, item = at + local;
             const bool live = item < items && group < groups;
-            float sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
             const int row = live ? item / kQuads : 0, c = live ? (item - row * kQuads) * 4 : 0;
+            float top = kLowestRef, total_l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
             if (live) {
-                float top = -INFINITY;
-                for (uint32_t i = 0; i < parts; i++) top = fmaxf(top, s_m[i * p.rows + row]);
-                for (uint32_t i = group; i < parts; i += groups) {
-                    const float f = __builtin_amdgcn_exp2f(s_m[i * p.rows + row] - top);
-                    const float *v = part_at(i) + row * kPitch + c;
-                    sum = fmaf(s_l[i * p.rows + row], f, sum);
+                for (uint32_t i = group; i < parts; i += 4 * groups) {
+                    float2 ml[4], lo[4], hi[4];
 #pragma unroll
-                    for (int x = 0; x < 4; x++) acc[x] = fmaf(load_agent(v + x), f, acc[x]);
+                    for (int x = 0; x < 4; x++) {
+                        const uint32_t part = min(i + x * groups, parts - 1);
+                        const float *v = p.a.partials + ((size_t)(2 * (from + part) + (part == 0 ? 1 : 0)) * p.rows + row) * kPitch;
+                        ml[x] = load_agent2(v + D);
+                        lo[x] = load_agent2(v + c);
+                        hi[x] = load_agent2(v + c + 2);
+                    }
+#pragma unroll
+                    for (int x = 0; x < 4; x++) {
+                        if (i + x * groups >= parts) continue;
+                        const float now = fmaxf(top, ml[x].x), old = __builtin_amdgcn_exp2f(top - now), f = __builtin_amdgcn_exp2f(ml[x].x - now);
+                        top = now;
+                        total_l = fmaf(ml[x].y, f, total_l * old);
+                        acc[0] = fmaf(lo[x].x, f, acc[0] * old);
+                        acc[1] = fmaf(lo[x].y, f, acc[1] * old);
+                        acc[2] = fmaf(hi[x].x, f, acc[2] * old);
+                        acc[3] = fmaf(hi[x].y, f, acc[3] * old);
+                    }
                 }
             }
-            if (groups > 1) {  // one round then: items < threads
-                *reinterpret_cast<float4 *>(s_dyn + 4 * tid) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+            if (groups > 1) {
+                float *mine = s_dyn + 6 * tid;
+                mine[0] = top; mine[1] = total_l; mine[2] = acc[0]; mine[3] = acc[1]; mine[4] = acc[2]; mine[5] = acc[3];
                 __syncthreads();
                 if (live && group == 0) {
                     for (int gr = 1; gr < groups; gr++) {
-                        const float4 v = *reinterpret_cast<const float4 *>(s_dyn + 4 * (gr * items + local));
-                        acc[0] += v.x; acc[1] += v.y; acc[2] += v.z; acc[3] += v.w;
+                        const float *v = s_dyn + 6 * (gr * items + local);
+                        const float now = fmaxf(top, v[0]), old = __builtin_amdgcn_exp2f(top - now), f = __builtin_amdgcn_exp2f(v[0] - now);
+                        top = now;
+                        total_l = fmaf(v[1], f, total_l * old);
+#pragma unroll
+                        for (int x = 0; x < 4; x++) acc[x] = fmaf(v[2 + x], f, acc[x] * old);
                     }
-                    float top = -INFINITY;
-                    for (uint32_t i = 0; i < parts; i++) top = fmaxf(top, s_m[i * p.rows + row]);
-                    sum = 0.f;
-                    for (uint32_t i = 0; i < parts; i++) sum = fmaf(s_l[i * p.rows + row], __builtin_amdgcn_exp2f(s_m[i * p.rows + row] - top), sum);
                 }
             }
-            if (live && group == 0) store_row4<T, D>(p, open_b[k], open_h[k], row, c, acc, sum);
+            if (live && group == 0) store_row4<T, D>(p, open_b[k], open_h[k], row, c, acc, total_l);
         }
         if (tid == 0) __hip_atomic_store(p.a.tickets + from, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
     }
 }
 
-template <int T, int C, int D, int R>
-hipError_t launch(const DecodeArgs &p, int max_len, hipStream_t s) {
-    constexpr int kThreads = 64 * decode_waves(R);
-    const size_t states = (size_t)2 * decode_waves(R) * p.rows * partial_pitch(D), join = (size_t)kThreads * 4 + 2 * (size_t)kDecodeWGs * p.rows;
+template <int T, int C, int D, int R, int W>
+hipError_t launch_waves(const DecodeArgs &p, int max_len, hipStream_t s) {
+    constexpr int kThreads = 64 * W;
+    const size_t states = (size_t)2 * W * p.rows * partial_pitch(D), join = (size_t)kThreads * 6;
     const size_t lds = 4 * ((states > join ? states : join) + p.g.batch + 1);
-    auto kernel = paged_decode_kernel<T, C, D, R>;
+    auto kernel = paged_decode_kernel<T, C, D, R, W>;
     static std::atomic<uint64_t> allowed{0};
     hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), kDecodeLdsBytes, allowed);
     if (e != hipSuccess) return e;
     if (lds > kDecodeLdsBytes) return hipErrorInvalidValue;
     // units of work that there could be: no more workgroups than they can busy
     const int pages = max_len > 0 && max_len < p.g.max_pages * kPBT ? (max_len + kPBT - 1) / kPBT : p.g.max_pages;
-    const size_t most = (size_t)p.g.batch * p.g.H * (pages + kTailUnits), per_wg = decode_waves(R) * kLeastUnits, wgs = (most + per_wg - 1) / per_wg;
+    const size_t most = (size_t)p.g.batch * p.g.H * (pages + kTailUnits), per_wg = W * kLeastUnits, wgs = (most + per_wg - 1) / per_wg;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(wgs < (size_t)kDecodeWGs ? wgs : (size_t)kDecodeWGs)), dim3(kThreads), lds, s, p);
     return hipGetLastError();
+}
+
+// Waves of a workgroup, one of which fills a CU: their states of two heads each have to fit the LDS, and twelve (or sixteen, for
+// heads of 64) with fewer registers each took 75 us instead of 56 over 32 heads x 32768 tokens and 23 to 28 instead of 21 over
+// 64 x 8 heads of up to 1100 (64 channels).
+template <int T, int C, int D, int R>
+hipError_t launch(const DecodeArgs &p, int max_len, hipStream_t s) {
+    return launch_waves<T, C, D, R, R == 1 ? 8 : 4>(p, max_len, s);
 }
 
 }  // namespace
