@@ -68,6 +68,7 @@ struct Wave {
     const DecodeArgs &p;
     const int lane, n, g4;
     half8v qf[R][KS];
+    uint4 qw[R][KS];
     float q_factor[R];
     int q_place[R];  // token of the row among the call's
     float m[R], l[R];
@@ -79,16 +80,24 @@ struct Wave {
         for (int r = 0; r < R; r++) q_place[r] = (16 * r + n) / p.g.G;
     }
 
-    __device__ __forceinline__ void begin(int b, int h) {
+    // A head's queries are asked for, and made ready once something else is on its way too.
+    __device__ __forceinline__ void ask_queries(int b, int h) {
 #pragma unroll
         for (int r = 0; r < R; r++) {
             const int row = 16 * r + n;
             const bool have = row < p.rows;
             const uint16_t *q = p.a.q + ((size_t)b * p.q_len + q_place[r]) * p.a.q_stride + (size_t)(h * p.g.G + row - q_place[r] * p.g.G) * D;
-            uint4 w[KS];
 #pragma unroll
             for (int k = 0; k < KS; k++)
-                w[k] = have ? *reinterpret_cast<const uint4 *>(q + (k >> 1) * 64 + g4 * 16 + (k & 1) * 8) : make_uint4(0, 0, 0, 0);
+                qw[r][k] = have ? *reinterpret_cast<const uint4 *>(q + (k >> 1) * 64 + g4 * 16 + (k & 1) * 8) : make_uint4(0, 0, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void begin() {
+#pragma unroll
+        for (int r = 0; r < R; r++) {
+            uint4 w[KS];
+#pragma unroll
+            for (int k = 0; k < KS; k++) w[k] = qw[r][k];
             q_factor[r] = 1.f;
             if constexpr (T == kBF16) {
                 uint32_t big = 0;
@@ -199,31 +208,32 @@ struct Wave {
         }
     }
 
-    // Pages [i0, whole) of a head whose first tile is `first`.
+    // Pages [i0, whole) of a head whose first tile is `first`; i0 < whole.
     __device__ __forceinline__ void run(int b, int h, int first, int i0, int whole, int len) {
-        if (i0 >= whole) return;
         const int32_t *pages = p.g.table + (size_t)b * p.g.max_pages + first;
         // page numbers and scales of 64 tiles, a tile a lane
         int known = i0, known_page = 0;
         float known_k = 0.f, known_v = 0.f;
-        auto learn = [&](int i) {
+        auto page_of = [&](int i) { return i + lane < whole ? pages[i + lane] : 0; };
+        auto learn = [&](int i, int page) {
             known = i;
-            if (i + lane < whole) {
-                known_page = pages[i + lane];
-                const bool ok = (unsigned)known_page < (unsigned)p.g.n_pages;
-                if (!ok) {
-                    flag(p.g.fault, kFaultPage);
-                    known_page = 0;
-                }
-                const float2 sc = *reinterpret_cast<const float2 *>(p.g.scales + ((size_t)known_page * p.g.H + h) * 2);
-                known_k = ok ? sc.x : kNan;
-                known_v = sc.y;
+            const bool ok = (unsigned)page < (unsigned)p.g.n_pages;
+            if (!ok) {
+                flag(p.g.fault, kFaultPage);
+                page = 0;
             }
+            known_page = page;
+            const float2 sc = *reinterpret_cast<const float2 *>(p.g.scales + ((size_t)page * p.g.H + h) * 2);
+            known_k = ok ? sc.x : kNan;
+            known_v = sc.y;
         };
         auto page_at = [&](int i) { return __builtin_amdgcn_readlane(known_page, i - known); };
-        learn(i0);
+        const int page0 = page_of(i0);
+        ask_queries(b, h);  // behind the page numbers, which are waited for first
+        learn(i0, page0);
         load_k(page_at(i0), h);
         load_v(page_at(i0), h);
+        begin();
         for (int i = i0; i < whole; i++) {
             float4v s[R][4];
 #pragma unroll
@@ -243,7 +253,7 @@ struct Wave {
             const float ks = bcast(known_k, i - known), vs = bcast(known_v, i - known);
             const bool more = i + 1 < whole;
             if (more) {
-                if (i + 1 == known + 64) learn(i + 1);
+                if (i + 1 == known + 64) learn(i + 1, page_of(i + 1));
                 load_k(page_at(i + 1), h);
             }
             float x[R][16], alpha[R];
@@ -258,9 +268,10 @@ struct Wave {
     }
 
     // The block that is still in 16 bits: K as it is, V turned in registers, rows behind the end left out.
-    __device__ __forceinline__ void unfinished(int b, int h, int len) {
+    __device__ __forceinline__ void unfinished(int b, int h, int len, int tail, bool alone) {
         const int count = len % kPBT;
-        const size_t at = ((size_t)uniform(p.g.tails[b]) * p.g.H + h) * kPBT * D;
+        const size_t at = ((size_t)tail * p.g.H + h) * kPBT * D;
+        if (alone) ask_queries(b, h);
         uint4 kt[4][KS];
         uint32_t vt[16][CT / 2];  // token 16 g4 + j, channels CT n ..
 #pragma unroll
@@ -280,6 +291,7 @@ struct Wave {
                 vt[j][0] = w.x; vt[j][1] = w.y;
             }
         }
+        if (alone) begin();
         float4v s[R][4];
 #pragma unroll
         for (int r = 0; r < R; r++) {
@@ -414,13 +426,15 @@ __global__ __launch_bounds__(64 * W) void paged_decode_kernel(DecodeArgs p) {
     auto pages_of = [&](int len) { return len / kPBT - tiles_of(len, p.q_len, p.a.window).first; };
     const bool few = p.g.batch <= 64;  // then a sequence is a lane, and nothing goes through LDS
     uint32_t sum = 0, lane_units = 0, lane_before = 0;
-    int lane_len = 0;
+    int lane_len = 0, lane_tail = 0;
     for (int base = 0; base < p.g.batch; base += 64) {
         lane_units = 0;
         if (base + lane < p.g.batch) {
             const int len = p.g.lens[base + lane], tail = p.g.tails[base + lane];
+            asm volatile("" ::"v"(tail));  // both are on their way at once
             if (sane(len, tail) && len > 0) lane_units = pages_of(len) + (len % kPBT ? kTailUnits : 0);
             lane_len = len;
+            lane_tail = tail;
         }
         lane_before = wave_excl_scan(lane_units, lane);
         if (!few && base + lane < p.g.batch) before[base + lane] = sum + lane_before;
@@ -431,21 +445,26 @@ __global__ __launch_bounds__(64 * W) void paged_decode_kernel(DecodeArgs p) {
     wave_sync();
     auto before_of = [&](int b) { return (uint32_t)(few ? __builtin_amdgcn_readlane((int)lane_before, b) : uniform((int)before[b])); };
     auto units_of = [&](int b) { return (uint32_t)(few ? __builtin_amdgcn_readlane((int)lane_units, b) : uniform((int)(before[b + 1] - before[b]))); };
-    // empty places: zeros; those that do not fit: NaN
-    for (int b = blockIdx.x; b < p.g.batch; b += gridDim.x) {
-        if (units_of(b) != 0) continue;
-        const int len = p.g.lens[b];
-        const bool ok = sane(len, p.g.tails[b]);
-        if (!ok && tid == 0) flag(p.g.fault, (unsigned)len <= (unsigned)p.g.max_pages * kPBT ? kFaultTail : kFaultLength);
-        const uint32_t w = ok ? 0u : kNanBits<T> * 0x10001u;
-        const int per_row = p.g.H * p.g.G * D / 8;
-        for (int i = tid; i < p.q_len * per_row; i += kThreads)
-            *reinterpret_cast<uint4 *>(p.a.out + ((size_t)b * p.q_len + i / per_row) * p.a.out_stride + (size_t)(i % per_row) * 8) = make_uint4(w, w, w, w);
-    }
+    // Empty places: zeros; those that do not fit: NaN.
+    auto fill_empty = [&]() {
+        for (int b = blockIdx.x; b < p.g.batch; b += gridDim.x) {
+            if (units_of(b) != 0) continue;
+            const int len = p.g.lens[b];
+            const bool ok = sane(len, p.g.tails[b]);
+            if (!ok && tid == 0) flag(p.g.fault, (unsigned)len <= (unsigned)p.g.max_pages * kPBT ? kFaultTail : kFaultLength);
+            const uint32_t w = ok ? 0u : kNanBits<T> * 0x10001u;
+            const int per_row = p.g.H * p.g.G * D / 8;
+            for (int i = tid; i < p.q_len * per_row; i += kThreads)
+                *reinterpret_cast<uint4 *>(p.a.out + ((size_t)b * p.q_len + i / per_row) * p.a.out_stride + (size_t)(i % per_row) * 8) = make_uint4(w, w, w, w);
+        }
+    };
     const uint32_t H = p.g.H, total = sum * H;
     // no more workgroups than there is work for their waves
     const uint32_t active = min((uint32_t)gridDim.x, (total + kWaves * kLeastUnits - 1) / (kWaves * kLeastUnits)), wg = blockIdx.x;
-    if (wg >= active) return;
+    if (wg >= active) {
+        fill_empty();
+        return;
+    }
     const Deal deal(total, active);
     const uint32_t wg_begin = deal.begin(wg), wg_end = deal.begin(wg + 1);
     const Deal inner(wg_end - wg_begin, kWaves);
@@ -477,9 +496,11 @@ __global__ __launch_bounds__(64 * W) void paged_decode_kernel(DecodeArgs p) {
         t += i1 - i0;
         const uint32_t pages = pages_of(len), tail = len % kPBT ? 1 : 0;
         if (i0 >= pages + tail) continue;  // the rest of an unfinished block's units: it belongs to the first one's owner
-        w.begin(b, (int)h);
-        w.run(b, (int)h, tiles_of(len, p.q_len, p.a.window).first, (int)min(i0, pages), (int)min(i1, pages), len);
-        if (tail && i0 <= pages && pages < i1) w.unfinished(b, (int)h, len);
+        if (i0 < pages) w.run(b, (int)h, tiles_of(len, p.q_len, p.a.window).first, (int)i0, (int)min(i1, pages), len);
+        if (tail && i0 <= pages && pages < i1) {
+            const int slot = few ? __builtin_amdgcn_readlane(lane_tail, b) : uniform(p.g.tails[b]);
+            w.unfinished(b, (int)h, len, slot, i0 == pages);
+        }
         if (i0 == 0 && i1 >= pages + tail) {
             w.store(b, (int)h);
         } else {
@@ -488,6 +509,7 @@ __global__ __launch_bounds__(64 * W) void paged_decode_kernel(DecodeArgs p) {
             parked++;
         }
     }
+    fill_empty();
     __syncthreads();
 
     // Join the parked states of each head; a head that other workgroups have a part of leaves its state in the workspace.
