@@ -41,6 +41,7 @@ struct PagedNew {
     const int32_t *__restrict__ positions;
     int n_positions, rot_dim, interleaved;
     int edge[2];  // first pair of the second and of the third axis
+    int stream_q;
 };
 
 // One attention call: queries and outputs [rows][Hq][D] with their strides in elements.

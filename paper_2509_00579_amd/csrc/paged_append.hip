@@ -81,6 +81,12 @@ __device__ __forceinline__ void store16(uint16_t *p, const uint32_t (&w)[4]) {
     *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// ... past the caches
+__device__ __forceinline__ void stream16(uint16_t *p, const uint32_t (&w)[4]) {
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    const u4 v = {w[0], w[1], w[2], w[3]};
+    __builtin_nontemporal_store(v, reinterpret_cast<u4 *>(p));
+}
 __device__ __forceinline__ uint32_t max16(uint32_t a, uint32_t b) {  // both halves, unsigned
     typedef unsigned short us2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, a), __builtin_bit_cast(us2, b)));
@@ -130,7 +136,8 @@ template <int C>
 constexpr float kMostCode = C == kI8 ? 127.f : 448.f;
 
 constexpr int kRowGroups = 16;   // four tokens each
-constexpr int kQRows = 4;        // rows of queries per thread
+// Rows of queries per thread (16421 tokens, 8 KV and 32 query heads, with 1, 2, 4, 8: 80.6 79.3 80 84 us).
+constexpr int kQRows = 2;
 constexpr int kVPitch = 17;      // words of a V channel in LDS: 16, and one so that the writers of eight channels hit eight banks
 
 template <int T, int C, int D>
@@ -147,47 +154,49 @@ __global__ __launch_bounds__(kRowGroups * D / 16) void paged_append_kernel(Paged
     c1 *= 8;
 
     if ((int)blockIdx.x >= block_units) {
-        // queries of chunks: four rows (token, head) per thread, neighbouring rows in neighbouring threads
+        // queries of chunks: kQRows rows (token, head) per thread, which are heads of one token where they go into a token's
+        // heads evenly; then its cosines and sines are read once
         const int Hq = g.H * g.G;
         const uint32_t rows = (uint32_t)n.n_tokens * (uint32_t)Hq;
-        const uint32_t r0 = (blockIdx.x - block_units) * (uint32_t)(kRowGroups * kQRows) + rg;
+        const uint32_t r0 = ((blockIdx.x - block_units) * (uint32_t)kRowGroups + rg) * kQRows;
+        const int n_first = n.starts[0], n_used = n.starts[g.batch];
         uint32_t x[kQRows][2][4];
-        uint32_t head[kQRows];
-        int tok[kQRows], pos[kQRows];
-        int b = 0;
-        const int n_used = n.starts[g.batch];
-        bool fine = true;
+        int tok[kQRows], head[kQRows];
 #pragma unroll
         for (int k = 0; k < kQRows; k++) {
-            const uint32_t r = r0 + k * kRowGroups;
-            tok[k] = r < rows ? (int)(r / (uint32_t)Hq) : 0x7fffffff;
-            head[k] = r - (uint32_t)tok[k] * (uint32_t)Hq;
-            pos[k] = 0;
-            if (tok[k] >= n_used || tok[k] < n.starts[0]) tok[k] = -1;
+            const uint32_t r = r0 + k;
+            tok[k] = (int)(r / (uint32_t)Hq);
+            head[k] = (int)(r - (uint32_t)tok[k] * (uint32_t)Hq);
+            if (r >= rows || tok[k] >= n_used || tok[k] < n_first) tok[k] = -1;
             if (tok[k] < 0) continue;
             const uint16_t *p = n.q + (size_t)tok[k] * n.q_stride + head[k] * D;
             load16(x[k][0], p + c0);
             load16(x[k][1], p + c1);
-            if (n.cos_sin && !n.positions) {
-                if (k == 0 || b == 0) {  // the last sequence that starts at or before the token
-                    int lo = 0, hi = g.batch;
-                    while (hi - lo > 1) {
-                        const int mid = (lo + hi) >> 1;
-                        if (n.starts[mid] <= tok[k]) lo = mid; else hi = mid;
-                    }
-                    b = lo;
-                } else {
-                    while (b + 1 < g.batch && n.starts[b + 1] <= tok[k]) b++;
-                }
-                pos[k] = g.lens[b] - n.starts[b + 1] + tok[k];
-            }
         }
+        bool fine = true, ok = true;
+        int b = -1;
+        Turn t;
 #pragma unroll
         for (int k = 0; k < kQRows; k++) {
             if (tok[k] < 0) continue;
             if (turned) {
-                Turn t;
-                const bool ok = load_turn(t, n, item, tok[k], pos[k]);
+                if (k == 0 || tok[k] != tok[k - 1]) {
+                    int pos = 0;
+                    if (!n.positions) {
+                        if (b < 0) {  // the last sequence that starts at or before the token
+                            int lo = 0, hi = g.batch;
+                            while (hi - lo > 1) {
+                                const int mid = (lo + hi) >> 1;
+                                if (n.starts[mid] <= tok[k]) lo = mid; else hi = mid;
+                            }
+                            b = lo;
+                        } else {
+                            while (b + 1 < g.batch && n.starts[b + 1] <= tok[k]) b++;
+                        }
+                        pos = g.lens[b] - n.starts[b + 1] + tok[k];
+                    }
+                    ok = load_turn(t, n, item, tok[k], pos);
+                }
                 turn<T>(x[k], t, n.interleaved);
                 if (!ok) {
                     x[k][0][0] = x[k][1][0] = kNanBits<T> * 0x10001u;
@@ -195,8 +204,13 @@ __global__ __launch_bounds__(kRowGroups * D / 16) void paged_append_kernel(Paged
                 }
             }
             uint16_t *p = n.q_out + (size_t)tok[k] * n.q_out_stride + head[k] * D;
-            store16(p + c0, x[k][0]);
-            store16(p + c1, x[k][1]);
+            if (n.stream_q) {
+                stream16(p + c0, x[k][0]);
+                stream16(p + c1, x[k][1]);
+            } else {
+                store16(p + c0, x[k][0]);
+                store16(p + c1, x[k][1]);
+            }
         }
         if (!fine) flag(g.fault, kFaultPosition);
         return;
@@ -417,11 +431,14 @@ __global__ __launch_bounds__(kRowGroups * D / 16) void paged_append_kernel(Paged
 }
 
 template <int T, int C, int D>
-void launch(const PagedGeo &g, const PagedNew &n, hipStream_t s) {
+void launch(const PagedGeo &g, PagedNew n, hipStream_t s) {
     // every sequence touches at most one block more than its new tokens fill, and one more where it starts inside a block
     const size_t units = n.starts ? (size_t)n.n_tokens / kPBT + 2 * (size_t)g.batch : (size_t)g.batch;
     const size_t most = n.starts && (size_t)n.n_tokens < units ? (size_t)n.n_tokens : units;
     const size_t q_rows = n.starts && n.q ? (size_t)n.n_tokens * g.H * g.G : 0;
+    // rotated queries that the L2s (8 x 4 MiB) cannot keep for the attention behind go past them: 79.3 -> 75.5 us for 134 MB, but
+    // 20.6 -> 21.8 for 19 MB
+    n.stream_q = q_rows * D * 2 > (size_t)32 << 20;
     const size_t q_units = (q_rows + kRowGroups * kQRows - 1) / (kRowGroups * kQRows);
     hipLaunchKernelGGL((paged_append_kernel<T, C, D>), dim3((unsigned)(most * g.H + q_units)), dim3(kRowGroups * D / 16), 0, s, g, n,
                        (int)(most * g.H));
