@@ -40,6 +40,7 @@ class Stats(C.Structure):
 
 # The paged cache's structures as packed bytes (native sizes and alignment): cheaper to make anew for every call than ctypes
 # structures, and a call's arguments stay its own when several threads call.
+_I32 = torch.int32
 _PAGED_CONFIG = struct.Struct("@8i")          # n_kv_heads n_q_heads head_dim data_type code_type n_pages n_tails max_pages
 _PAGED_CACHE = struct.Struct("@6P")           # k_codes v_codes scales k_tail v_tail fault
 _PAGED_BATCH = struct.Struct("@i3P")          # batch lens table tails
@@ -429,26 +430,26 @@ class PagedCache:
         return cfg
 
     def _batch(self, lens, table, tails):
-        i32, dev, n = torch.int32, self._index, lens.shape[0]
-        assert lens.dtype is i32 and table.dtype is i32 and tails.dtype is i32, "lens, table and tails are int32"
-        assert lens.get_device() == dev and table.get_device() == dev and tails.get_device() == dev, (
-            f"lens, table and tails must be on {self.device}")
-        assert lens.dim() == 1 and table.dim() == 2 and table.shape[0] == n and tails.dim() == 1 and tails.shape[0] == n, "one row per sequence"
+        """The packed sequences, their number and the configuration that goes with the table's width."""
+        shape, wide = lens.shape, table.shape
+        assert lens.dtype is _I32 and table.dtype is _I32 and tails.dtype is _I32, "lens, table and tails are int32"
+        assert lens.get_device() == table.get_device() == tails.get_device() == self._index, f"lens, table and tails must be on {self.device}"
+        assert len(shape) == 1 and tails.shape == shape and len(wide) == 2 and wide[0] == shape[0], "one row per sequence"
         assert table.is_contiguous() and lens.is_contiguous() and tails.is_contiguous(), "lens, table and tails must be contiguous"
-        return _PAGED_BATCH.pack(n, lens.data_ptr(), table.data_ptr(), tails.data_ptr())
+        return _PAGED_BATCH.pack(shape[0], lens.data_ptr(), table.data_ptr(), tails.data_ptr()), shape[0], self._cfg(wide[1])
 
     def _starts(self, starts, batch):
-        assert starts.dtype is torch.int32 and starts.get_device() == self._index and starts.is_contiguous()
-        assert starts.dim() == 1 and starts.shape[0] == batch + 1, "starts: one entry per sequence and the end"
+        assert starts.dtype is _I32 and starts.get_device() == self._index and starts.is_contiguous()
+        assert starts.shape == (batch + 1,), "starts: one entry per sequence and the end"
         return starts.data_ptr()
 
-    def _rows(self, x, n, heads, name):
+    def _rows(self, x, shape, name):
         """Pointer and token stride of a tensor [n, heads, head_dim] whose tokens may be apart (a slice of a fused projection)."""
         assert x.get_device() == self._index and x.dtype is self.dtype, f"{name} must be {self.dtype} on {self.device}"
-        assert x.shape == (n, heads, self.D), f"{name}: expected shape {(n, heads, self.D)}, got {tuple(x.shape)}"
+        assert x.shape == shape, f"{name}: expected shape {shape}, got {tuple(x.shape)}"
         s0, s1, s2 = x.stride()
-        assert s2 == 1 and (s1 == self.D or heads == 1), f"the heads of a token of {name} must be contiguous"
-        return x.data_ptr(), s0 if n > 1 else heads * self.D
+        assert s2 == 1 and (s1 == shape[2] or shape[1] == 1), f"the heads of a token of {name} must be contiguous"
+        return x.data_ptr(), s0 if shape[0] > 1 else shape[1] * shape[2]
 
     def _on_device(self):
         if torch._C._cuda_getDevice() != self._index:
@@ -462,18 +463,20 @@ class PagedCache:
         Returns q_out."""
         stream = self._on_device()
         n = k.shape[0]
-        seqs = self._batch(lens, table, tails)
-        kp, ks = self._rows(k, n, self.H, "k")
-        vp, vs = self._rows(v, n, self.H, "v")
+        seqs, batch, cfg = self._batch(lens, table, tails)
+        shape = (n, self.H, self.D)
+        kp, ks = self._rows(k, shape, "k")
+        vp, vs = self._rows(v, shape, "v")
         sp = qp = qs = op = os_ = cp = n_pos = rot = inter = pp = 0
         axes, sections = 1, (0, 0, 0)
         if starts is not None:
-            sp = self._starts(starts, lens.shape[0])
+            sp = self._starts(starts, batch)
         if q is not None:
             if q_out is None:
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            qp, qs = self._rows(q, n, self.Hq, "q")
-            op, os_ = self._rows(q_out, n, self.Hq, "q_out")
+            shape = (n, self.Hq, self.D)
+            qp, qs = self._rows(q, shape, "q")
+            op, os_ = self._rows(q_out, shape, "q_out")
         if rope is not None:
             assert rope.cos_sin.get_device() == self._index
             cp, n_pos, rot, inter, axes, sections = (rope.cos_sin.data_ptr(), rope.n_positions, rope.rot_dim, rope.interleaved,
@@ -483,7 +486,7 @@ class PagedCache:
                 assert positions.shape == (axes, n), f"positions: expected shape {(axes, n)}, got {tuple(positions.shape)}"
                 pp = positions.data_ptr()
         new = _PAGED_NEW.pack(n, sp, kp, vp, ks, vs, qp, op, qs, os_, cp, n_pos, rot, inter, axes, *sections, pp)
-        st = self.lib.kvcomp_paged_append(self._cfg(table.shape[1]), self._memory, seqs, new, stream)
+        st = self.lib.kvcomp_paged_append(cfg, self._memory, seqs, new, stream)
         if st:
             _check(st)
         return q_out
@@ -504,14 +507,14 @@ class PagedCache:
         """Attention of q [batch * q_len, n_q_heads, head_dim], the last q_len tokens of every sequence, over the cache;
         window: keys that a token sees, itself included (0: all before it); max_len: the longest length, if known."""
         stream = self._on_device()
-        seqs = self._batch(lens, table, tails)
-        n = lens.shape[0] * q_len
+        seqs, batch, cfg = self._batch(lens, table, tails)
+        shape = (batch * q_len, self.Hq, self.D)
         if out is None:
-            out = torch.empty((n, self.Hq, self.D), dtype=self.dtype, device=self.device)
-        qp, qs = self._rows(q, n, self.Hq, "q")
-        op, os_ = self._rows(out, n, self.Hq, "out")
+            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+        qp, qs = self._rows(q, shape, "q")
+        op, os_ = self._rows(out, shape, "out")
         ws = self._scratch(workspace)
-        _check(self.lib.kvcomp_paged_attn_decode(self._cfg(table.shape[1]), self._memory, seqs, qp, qs, q_len, float(scale), window,
+        _check(self.lib.kvcomp_paged_attn_decode(cfg, self._memory, seqs, qp, qs, q_len, float(scale), window,
                                                  max_len, op, os_, ws.data_ptr(), ws.numel(), stream))
         return out
 
@@ -519,15 +522,16 @@ class PagedCache:
         """Attention of chunks: rows starts[b] .. starts[b + 1] of q [n, n_q_heads, head_dim] are the last tokens of sequence b
         (starts: int32 [batch + 1]); max_new, max_len: the longest chunk and length, if known."""
         stream = self._on_device()
-        seqs = self._batch(lens, table, tails)
-        sp = self._starts(starts, lens.shape[0])
+        seqs, batch, cfg = self._batch(lens, table, tails)
+        sp = self._starts(starts, batch)
         n = q.shape[0]
+        shape = (n, self.Hq, self.D)
         if out is None:
-            out = torch.empty((n, self.Hq, self.D), dtype=self.dtype, device=self.device)
-        qp, qs = self._rows(q, n, self.Hq, "q")
-        op, os_ = self._rows(out, n, self.Hq, "out")
+            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+        qp, qs = self._rows(q, shape, "q")
+        op, os_ = self._rows(out, shape, "out")
         ws = self._scratch(workspace)
-        _check(self.lib.kvcomp_paged_attn_prefill(self._cfg(table.shape[1]), self._memory, seqs, qp, qs, sp, n,
+        _check(self.lib.kvcomp_paged_attn_prefill(cfg, self._memory, seqs, qp, qs, sp, n,
                                                   float(scale), window, max_new, max_len, op, os_, ws.data_ptr(), ws.numel(), stream))
         return out
 
