@@ -396,10 +396,11 @@ class PagedCache:
     The pages, scales and tails are tensors of the caller's, `storage` = (k_codes, v_codes, scales, k_tail, v_tail), or are
     allocated here.  Which sequence has which pages and tail, and how long it is, comes with every call: lens [batch], table
     [batch, max_pages] and tails [batch] are int32 CUDA tensors, read on the device.  lens counts the call's own tokens.
-    Calls on one cache from several streams at a time need a workspace each (new_workspace)."""
+    `workspace` is the attention calls' scratch, a cache's own if None; caches whose calls never overlap in time (the layers of
+    a model on one stream) may share one, calls on several streams at a time need one each (new_workspace)."""
 
     def __init__(self, n_kv_heads, n_q_heads, n_pages, n_tails, head_dim=D, dtype=torch.float16, codes="int8", device="cuda:0",
-                 storage=None):
+                 storage=None, workspace=None):
         self.lib = load()
         self.device = torch.device(device)
         if self.device.index is None:
@@ -421,7 +422,7 @@ class PagedCache:
         self._memory = _PAGED_CACHE.pack(*(x.data_ptr() for x in (*storage, self.fault)))
         self._index = self.device.index
         self._config = {}
-        self._workspace = None
+        self._workspace = self.new_workspace() if workspace is None else self._scratch(workspace)
 
     def _cfg(self, max_pages):
         cfg = self._config.get(max_pages)
@@ -496,10 +497,6 @@ class PagedCache:
         return torch.zeros(self.lib.kvcomp_paged_workspace_bytes(self._cfg(1)), dtype=torch.uint8, device=self.device)
 
     def _scratch(self, workspace):
-        if workspace is None:
-            if self._workspace is None:
-                self._workspace = self.new_workspace()
-            return self._workspace
         assert workspace.get_device() == self._index and workspace.dtype is torch.uint8 and workspace.is_contiguous()
         return workspace
 
@@ -513,7 +510,7 @@ class PagedCache:
             out = torch.empty(shape, dtype=self.dtype, device=self.device)
         qp, qs = self._rows(q, shape, "q")
         op, os_ = self._rows(out, shape, "out")
-        ws = self._scratch(workspace)
+        ws = self._workspace if workspace is None else self._scratch(workspace)
         _check(self.lib.kvcomp_paged_attn_decode(cfg, self._memory, seqs, qp, qs, q_len, float(scale), window,
                                                  max_len, op, os_, ws.data_ptr(), ws.numel(), stream))
         return out
@@ -530,7 +527,7 @@ class PagedCache:
             out = torch.empty(shape, dtype=self.dtype, device=self.device)
         qp, qs = self._rows(q, shape, "q")
         op, os_ = self._rows(out, shape, "out")
-        ws = self._scratch(workspace)
+        ws = self._workspace if workspace is None else self._scratch(workspace)
         _check(self.lib.kvcomp_paged_attn_prefill(cfg, self._memory, seqs, qp, qs, sp, n,
                                                   float(scale), window, max_new, max_len, op, os_, ws.data_ptr(), ws.numel(), stream))
         return out

@@ -38,9 +38,16 @@ __device__ __forceinline__ float4v product(uint4 a, uint4 b, float4v c) {
     if constexpr (T == kBF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
     else return mfma16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c);
 }
-__device__ __forceinline__ uint4 half8_to_bf16(half8v v) {
-    return make_uint4(narrow2<kBF16>((float)v[0], (float)v[1]), narrow2<kBF16>((float)v[2], (float)v[3]),
-                      narrow2<kBF16>((float)v[4], (float)v[5]), narrow2<kBF16>((float)v[6], (float)v[7]));
+// Queries for products with keys that are still in 16 bits.  bf16 ones come back from fp16 exactly, their largest between 1 and 2, so
+// that no key overflows a product that binary32 could hold.
+constexpr float kBackFromHalf = 6.103515625e-05f;  // 2^-14
+template <int T>
+__device__ __forceinline__ uint4 raw_queries(half8v v) {
+    if constexpr (T == kF16) return __builtin_bit_cast(uint4, v);
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; k++) w[k] = narrow2<kBF16>((float)v[2 * k] * kBackFromHalf, (float)v[2 * k + 1] * kBackFromHalf);
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -268,7 +275,7 @@ struct Wave {
         }
     }
 
-    // The block that is still in 16 bits: K as it is, V turned in registers, rows behind the end left out.
+    // The block that is still in 16 bits, on products of its own type: K as it is, V turned in registers, rows behind the end left out.
     __device__ __forceinline__ void unfinished(int b, int h, int len, int tail, bool alone) {
         const int count = len % kPBT;
         const size_t at = ((size_t)tail * p.g.H + h) * kPBT * D;
@@ -296,9 +303,9 @@ struct Wave {
         float4v s[R][4];
 #pragma unroll
         for (int r = 0; r < R; r++) {
-            uint4 qt[KS];  // bf16 queries are exact in both types
+            uint4 qt[KS];
 #pragma unroll
-            for (int x = 0; x < KS; x++) qt[x] = T == kBF16 ? half8_to_bf16(qf[r][x]) : __builtin_bit_cast(uint4, qf[r][x]);
+            for (int x = 0; x < KS; x++) qt[x] = raw_queries<T>(qf[r][x]);
 #pragma unroll
             for (int t = 0; t < 4; t++) {
                 s[r][t] = float4v{0.f, 0.f, 0.f, 0.f};
@@ -309,13 +316,13 @@ struct Wave {
         float x[R][16], alpha[R];
         constexpr int kParts = T == kBF16 ? 3 : 2;  // of 8 and of 11 bits
         uint32_t parts[R][kParts][8];
-        scores(s, p.a.scale, len - count, len, x);
+        scores(s, T == kBF16 ? p.a.scale / kBackFromHalf : p.a.scale, len - count, len, x);
 #pragma unroll
         for (int r = 0; r < R; r++) {
             alpha[r] = weigh(r, x[r]);
 #pragma unroll
             for (int j = 0; j < 16; j += 2) {
-                float a = x[r][j], c = x[r][j + 1];
+                float a = x[r][j] * kVUnit<T>, c = x[r][j + 1] * kVUnit<T>;  // bf16 has the exponents for it
 #pragma unroll
                 for (int k = 0; k < kParts; k++) {
                     const uint32_t w = narrow2<T>(a, c);
@@ -345,7 +352,7 @@ struct Wave {
                         acc = product<T>(make_uint4(a[4 * h8], a[4 * h8 + 1], a[4 * h8 + 2], a[4 * h8 + 3]),
                                          make_uint4(parts[r][k][4 * h8], parts[r][k][4 * h8 + 1], parts[r][k][4 * h8 + 2], parts[r][k][4 * h8 + 3]), acc);
 #pragma unroll
-                for (int k = 0; k < 4; k++) o[r][c][k] = fmaf(acc[k], kVUnit<T>, o[r][c][k] * alpha[r]);
+                for (int k = 0; k < 4; k++) o[r][c][k] = fmaf(o[r][c][k], alpha[r], acc[k]);
             }
         }
     }

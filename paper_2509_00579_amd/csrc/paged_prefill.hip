@@ -11,6 +11,9 @@
 // of it (int8) or 2^-15 (e4m3), off by 2^-25 of the largest scale below that.  So a tile's product adds to the output's
 // accumulators as it is.  P is rounded to fp16 (11 bits, relative to each weight: the reference leaves 2^8 to 2^14 above
 // one, so weights down to 2^-22 of a row's largest keep all of them), and the sum of the weights is taken from the rounded ones.
+// The exponent is one fused product of the score's factors minus the reference, which was rounded: all weights of a row are off
+// by one common factor, which the division takes out, as long as it is neither 0 nor infinite; rows with scores beyond 2^26
+// are refused for that (NaN, and a flag).
 // The reference moves only when a score would pass 2^14 above it, which spares most tiles the rescaling of the accumulators.
 //
 // Few rows over a long axis: the keys are split among workgroups, and a second launch joins their states.
@@ -25,7 +28,7 @@ namespace kvc {
 
 namespace {
 
-constexpr float kRefLead = 8.f, kRefMost = 14.f;
+constexpr float kRefLead = 8.f, kRefMost = 14.f, kFarScore = 67108864.f;
 
 struct PrefillArgs {
     PagedGeo g;
@@ -43,42 +46,42 @@ constexpr int workgroups_per_cu(int D, int W) { return W == 8 ? 1 : D == 128 ? 2
 
 // The row tile of a unit: which sequence, its first token among the sequence's new ones.
 struct RowTile {
-    int b, start, fresh, len, place;
+    int b, start, fresh, len, tail, place;
     bool bad;
 };
-// All lanes of a wave together.  b < 0: no such unit.
+// All lanes of a wave together.  b < 0: no such unit.  Everything that is read of 64 sequences is on its way at once.
 __device__ __forceinline__ RowTile find_tile(const PrefillArgs &p, int unit, int lane) {
     RowTile r;
     r.b = -1;
-    r.bad = false;
-    for (int base = 0; base < p.g.batch && r.b < 0; base += 64) {
-        int tiles = 0;
+    for (int base = 0; base < p.g.batch; base += 64) {
+        int tiles = 0, s0 = 0, s1 = 0, len = 0, tail = 0;
         if (base + lane < p.g.batch) {
-            const int s0 = p.starts[base + lane], s1 = p.starts[base + lane + 1];
+            s0 = p.starts[base + lane];
+            s1 = p.starts[base + lane + 1];
+            len = p.g.lens[base + lane];
+            tail = p.g.tails[base + lane];
+            asm volatile("" ::"v"(len), "v"(tail));
             if (s0 >= 0 && s1 > s0 && s1 <= p.n_tokens) tiles = (s1 - s0 + p.per_tile - 1) / p.per_tile;
             else if (s1 != s0 || s0 < 0 || s1 > p.n_tokens) flag(p.g.fault, kFaultLength);
         }
         const int before = (int)wave_excl_scan((uint32_t)tiles, lane);
         const unsigned long long past = __builtin_amdgcn_ballot_w64(before + tiles > unit);
-        if (past) {
-            const int at = __builtin_ctzll(past);
-            r.b = base + at;
-            r.place = uniform(unit - __builtin_amdgcn_readlane(before, at)) * p.per_tile;
-        } else {
+        if (r.b >= 0) continue;
+        if (!past) {
             unit -= __builtin_amdgcn_readlane(before + tiles, 63);
+            continue;
         }
-    }
-    r.b = uniform(r.b);
-    if (r.b < 0) return r;
-    r.start = uniform(p.starts[r.b]);
-    r.fresh = uniform(p.starts[r.b + 1]) - r.start;
-    r.len = uniform(p.g.lens[r.b]);
-    if ((unsigned)r.len > (unsigned)p.g.max_pages * kPBT) {
-        r.bad = true;
-        if (lane == 0) flag(p.g.fault, kFaultLength);
-    } else if (r.len % kPBT && (unsigned)p.g.tails[r.b] >= (unsigned)p.g.n_tails) {
-        r.bad = true;
-        if (lane == 0) flag(p.g.fault, kFaultTail);
+        const int at = uniform(__builtin_ctzll(past));
+        r.b = base + at;
+        r.place = uniform(unit - __builtin_amdgcn_readlane(before, at)) * p.per_tile;
+        r.start = __builtin_amdgcn_readlane(s0, at);
+        r.fresh = __builtin_amdgcn_readlane(s1, at) - r.start;
+        r.len = __builtin_amdgcn_readlane(len, at);
+        r.tail = __builtin_amdgcn_readlane(tail, at);
+        const bool long_ = (unsigned)r.len > (unsigned)p.g.max_pages * kPBT, no_tail = r.len % kPBT && (unsigned)r.tail >= (unsigned)p.g.n_tails;
+        r.bad = long_ || no_tail;
+        if (r.bad && lane == 0) flag(p.g.fault, long_ ? kFaultLength : kFaultTail);
+        if (blockIdx.x) break;  // the first workgroup looks at all sequences
     }
     return r;
 }
@@ -215,6 +218,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
     const int wave_first = uniform(past + rt.place + 32 * wave / G);
     auto some_hidden = [&](int t) { return t * kPBT + kPBT - 1 > wave_first || (p.a.window > 0 && t * kPBT <= wave_last - p.a.window); };
 
+    bool far = false;  // my row has met a score that is refused
     float16v s[2];       // scores
     uint32_t pw[2][8];   // weights, fp16
     auto rescale = [&](float by) __attribute__((always_inline)) {
@@ -270,6 +274,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         if (__builtin_amdgcn_ballot_w64(move) != 0 || by_e != 1.f) {
             const float ref = move ? fmaxf(mx, kLowestRef) - kRefLead : st.ref;
             const float alpha = move ? __builtin_amdgcn_exp2f(st.ref - ref) : 1.f;
+            far = far || (move && fabsf(ref) > kFarScore);  // a score above the reference's lead moves it
             st.ref = ref;
             st.sum *= alpha;
             rescale(alpha * by_e);
@@ -423,7 +428,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         // the block that is still in 16 bits: K as it is (bf16: times a power of two), V turned and brought to the accumulators' unit
         const int t = unfinished, count = rt.len - t * kPBT;
         uint4 *sk = s_tiles, *sv = sk + kUnits;
-        const size_t at = ((size_t)uniform(p.g.tails[rt.b]) * p.g.H + h) * kPBT * D;
+        const size_t at = ((size_t)rt.tail * p.g.H + h) * kPBT * D;
         constexpr int kRowUnits = D / 8, kMine = kUnits / kPreThreads;
         uint32_t bk = 0, bv = 0;
         auto largest = [](uint32_t m, uint4 v) {
@@ -491,9 +496,11 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         sum = __uint_as_float(both[0]) + __uint_as_float(both[1]);
     }
     e_ref = max(e_ref, -140);  // still there where nothing was met
+    const bool refused = rt.bad || far;
+    if (live && far) flag(p.g.fault, kFaultScore);
     if (p.splits == 1) {
         if (!live) return;
-        const float f = rt.bad ? __builtin_nanf("") : sum == 0.f ? 0.f : 1.f / sum, unit_v = ldexpf(1.f, e_ref);
+        const float f = refused ? __builtin_nanf("") : sum == 0.f ? 0.f : 1.f / sum, unit_v = ldexpf(1.f, e_ref);
 #pragma unroll
         for (int c = 0; c < D / 32; c++) st.o[c] *= f;  // first: with their unit they could be too large
         store_rows<T, D>(p.a.out + (size_t)(rt.start + place) * p.a.out_stride + (size_t)head * D, half, st, unit_v);
@@ -509,7 +516,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
                 make_float4(st.o[c][i], st.o[c][i + 1], st.o[c][i + 2], st.o[c][i + 3]);
     if (half == 0) {
         part[D] = st.ref;
-        part[D + 1] = rt.bad ? __builtin_nanf("") : sum;
+        part[D + 1] = refused ? __builtin_nanf("") : sum;
         part[D + 2] = (float)e_ref;
     }
 }
@@ -571,16 +578,17 @@ hipError_t launch_tiles(PrefillArgs p, int max_len, hipStream_t s) {
     p.units = p.n_tokens / p.per_tile + some;
     const long long base = (long long)p.units * p.g.H;
     const int pages = max_len > 0 && max_len < p.g.max_pages * kPBT ? (max_len + kPBT - 1) / kPBT : p.g.max_pages;
-    // Splits of the keys, by what they would take in blocks per workgroup: as many rounds as the workgroups that there are likely
-    // to be need, at least the longest one, and what a split costs by itself (its state's way to memory and back).
-    const double tiles = (double)((p.n_tokens + p.per_tile - 1) / p.per_tile + (some - 1) / 2) * p.g.H;
+    // Splits of the keys, by what they would take in blocks per CU: the row tiles that there are likely to be, in rounds where one
+    // workgroup fills a CU (several share its time evenly), at least the longest one, and what a split costs by itself (its
+    // state's way to memory and back).  4 chunks of 16 tokens on 4001, 8 KV heads, groups of 4, with 4, 6, 8, 12, 15, 20 splits:
+    // 39.7 33.0 29.3 32.4 30.7 38.3 us.
+    const double tiles = std::max<double>(some, (p.n_tokens + p.per_tile - 1) / p.per_tile + 0.5 * (some - 1)) * p.g.H;
     const double longest = p.a.window > 0 ? std::min<double>(pages, (p.a.window + p.per_tile) / kPBT + 2) : pages;
     const double mean = std::max(longest / 2, longest - (double)p.n_tokens / some / kPBT / 2);
-    const int slots = 256 * workgroups_per_cu(D, W);
     double best = 0;
     p.splits = 1;
     for (int k = 1; k <= kMaxKeySplits && (k == 1 || (k * 4 <= longest && base * k * 32 * W <= kPrefillStateRows)); k++) {
-        const double rounds = std::max(1.0, std::ceil(tiles * k / slots)), extra = k == 1 ? 0 : 3 * rounds + 6 + 0.1 * k;
+        const double share = tiles * k / 256, rounds = std::max(1.0, workgroups_per_cu(D, W) == 1 ? std::ceil(share) : share), extra = k == 1 ? 0 : 3 * rounds + 6 + 0.1 * k;
         const double cost = std::max(rounds * mean / k, longest / k) + extra;
         if (k == 1 || cost < best) {
             best = cost;

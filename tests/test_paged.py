@@ -390,6 +390,22 @@ def test_decode_split_over_waves_and_workgroups(gpu, batch, H, G, longest):
     assert torch.equal(a, c) and not ws[:4096].any()
 
 
+def test_caches_that_share_a_workspace(gpu):
+    """Layers on one stream: decode and prefill calls of two caches in turn on one scratch."""
+    one = World(gpu, 3, 2, 2, 64, torch.float16, "int8", 30, seed=2)
+    two = World(gpu, 2, 1, 8, 64, torch.float16, "e4m3", 40, seed=3)
+    two.cache._workspace = one.cache._workspace
+    for w, counts in ((one, [1800, 3, 900]), (two, [2400, 70])):
+        k, v, _ = w.tokens(sum(counts))
+        w.append(counts, k, v)
+    for _ in range(2):
+        for w in (one, two):
+            _decode(w, 1)
+            _prefill(w, [3] * w.batch, max_new=3)
+    shared = gpu.PagedCache(2, 4, 8, 2, workspace=one.cache.new_workspace())
+    assert shared._workspace.numel() >= one.cache._workspace.numel()
+
+
 def test_decode_strides_and_rows_behind_the_batch(gpu):
     w = World(gpu, 3, 2, 2, 64, torch.bfloat16, "int8", 3, seed=2)
     counts = [70, 64, 10]
@@ -611,8 +627,30 @@ def test_attention_at_the_ends_of_the_range_of_bf16(gpu):
     v[150:] = (v[150:].double() * 1e-28).to(torch.bfloat16)
     w.append([150, 150], k, v)
     _decode(w, 1)
+    _decode(w, 4)
     _prefill(w, [150, 150])
     _prefill(w, [3, 3])
+    # keys whose products with the queries binary32 just holds: one of them takes all the weight
+    w = World(gpu, 2, 1, 2, 64, torch.bfloat16, "e4m3", 3, seed=3)
+    k, v, _ = w.tokens(2 * 150)
+    k = (k.double() * 1e34).to(torch.bfloat16)
+    w.append([150, 150], k, v)
+    q = w.rand(6, 2, 64).to(torch.bfloat16)
+    got = w.cache.attn_decode(q.cuda(), 0.125, _i32(w.lens), w.d_table, w.d_tails, q_len=3)
+    _close(got, *_reference(w, [3, 3], 0, 0.125, q), w.dtype)
+    w.cache.check()
+    got = w.cache.attn_prefill(q.cuda(), 0.125, _starts([3, 3]), _i32(w.lens), w.d_table, w.d_tails)
+    assert torch.isnan(got).all()  # refused, and said so
+    with pytest.raises(gpu.KvcompError) as e:
+        w.cache.check()
+    assert e.value.status == gpu.ERR_STATE
+    # scores up to 2^25 are taken (an error of theirs is a common factor of a row's weights, or lies within `spread`)
+    w = World(gpu, 2, 1, 2, 64, torch.bfloat16, "e4m3", 3, seed=3)
+    k, v, _ = w.tokens(2 * 150)
+    k = (k.double() * 1e5).to(torch.bfloat16)
+    w.append([150, 150], k, v)
+    _prefill(w, [150, 150])
+    w.cache.check()
 
 
 @pytest.mark.parametrize("D", [64, 128])
