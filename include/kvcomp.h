@@ -345,8 +345,7 @@ kvcomp_status kvcomp_paged_attn_decode(const kvcomp_paged_config *cfg, const kvc
  * row at that position sees.  d_q, d_out: DEVICE [n_tokens][n_q_heads][head_dim]; rows of d_out outside every sequence's
  * range, and those of a sequence whose starts do not fit into n_tokens, are left as they were.  max_new, max_len: the most new
  * tokens and the longest length as far as the caller knows (0: no idea); they shape the launch only.  One kernel, and a
- * second one where few rows over long sequences make it split the keys.  Rows with a score (scale * q.k * log2(e)) beyond
- * 2^26 in magnitude are refused: NaN, and reported by kvcomp_paged_check.  Errors: INVALID_ARG, CAPACITY, HIP. */
+ * second one where few rows over long sequences make it split the keys.  Errors: INVALID_ARG, CAPACITY, HIP. */
 kvcomp_status kvcomp_paged_attn_prefill(const kvcomp_paged_config *cfg, const kvcomp_paged_cache *cache,
                                         const kvcomp_paged_batch *seqs, const void *d_q, size_t q_stride, const void *d_starts,
                                         int n_tokens, float scale, int window, int max_new, int max_len, void *d_out,
@@ -354,8 +353,8 @@ kvcomp_status kvcomp_paged_attn_prefill(const kvcomp_paged_config *cfg, const kv
 
 /* What kernels flagged since the last check, once, and in this order: a page, tail or position out of range, or lengths or
  * starts that do not fit (STATE: such a sequence's tokens were not stored, its output rows are NaN; a token at a position
- * outside the table counts as one that holds NaN), a score that kvcomp_paged_attn_prefill does not take (STATE), Inf or NaN
- * in what was appended (NONFINITE).  SYNCHRONISES `stream` and clears the flags. */
+ * outside the table counts as one that holds NaN), Inf or NaN in what was appended (NONFINITE).  SYNCHRONISES `stream` and
+ * clears the flags. */
 kvcomp_status kvcomp_paged_check(const kvcomp_paged_cache *cache, void *stream);
 
 const char *kvcomp_last_error(void);

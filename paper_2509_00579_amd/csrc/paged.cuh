@@ -15,7 +15,7 @@ enum : int { kF16 = 0, kBF16 = 1 };
 enum : int { kI8 = 0, kE4M3 = 1 };
 
 // Flags in the cache's fault word.
-constexpr uint32_t kFaultPage = 1u, kFaultTail = 2u, kFaultPosition = 4u, kFaultLength = 8u, kFaultNonfinite = 16u, kFaultScore = 32u;
+constexpr uint32_t kFaultPage = 1u, kFaultTail = 2u, kFaultPosition = 4u, kFaultLength = 8u, kFaultNonfinite = 16u;
 
 // Cache and sequences of one call, by value to the kernels.
 struct PagedGeo {

@@ -195,7 +195,6 @@ kvcomp_status kvcomp_paged_check(const kvcomp_paged_cache *cache, void *stream) 
     if (fault & kFaultTail) return fail(KVCOMP_ERR_STATE, "a tail that was needed is outside the cache");
     if (fault & kFaultLength) return fail(KVCOMP_ERR_STATE, "a length or a start does not fit");
     if (fault & kFaultPosition) return fail(KVCOMP_ERR_STATE, "a position is outside the table of cosines and sines");
-    if (fault & kFaultScore) return fail(KVCOMP_ERR_STATE, "a prompt chunk's attention met a score beyond 2^26");
     return fail(KVCOMP_ERR_NONFINITE, "an appended token held Inf or NaN");
 }
 

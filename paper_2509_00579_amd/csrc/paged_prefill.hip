@@ -12,8 +12,8 @@
 // accumulators as it is.  P is rounded to fp16 (11 bits, relative to each weight: the reference leaves 2^8 to 2^14 above
 // one, so weights down to 2^-22 of a row's largest keep all of them), and the sum of the weights is taken from the rounded ones.
 // The exponent is one fused product of the score's factors minus the reference, which was rounded: all weights of a row are off
-// by one common factor, which the division takes out, as long as it is neither 0 nor infinite; rows with scores beyond 2^26
-// are refused for that (NaN, and a flag).
+// by one common factor, which the division takes out as long as it is neither 0 nor infinite; from scores of 2^26 on it
+// could be, and the product is rounded by itself.
 // The reference moves only when a score would pass 2^14 above it, which spares most tiles the rescaling of the accumulators.
 //
 // Few rows over a long axis: the keys are split among workgroups, and a second launch joins their states.
@@ -218,7 +218,6 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
     const int wave_first = uniform(past + rt.place + 32 * wave / G);
     auto some_hidden = [&](int t) { return t * kPBT + kPBT - 1 > wave_first || (p.a.window > 0 && t * kPBT <= wave_last - p.a.window); };
 
-    bool far = false;  // my row has met a score that is refused
     float16v s[2];       // scores
     uint32_t pw[2][8];   // weights, fp16
     auto rescale = [&](float by) __attribute__((always_inline)) {
@@ -246,7 +245,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
     };
     // Scores of block t to weights; mant: log2 of its V scale's mantissa, inv: one over that mantissa, by_e brings the accumulators to the unit that V is staged in.
     auto weigh = [&](int t, float k_scale, float mant, float inv, float by_e, bool masked) __attribute__((always_inline)) {
-        const float f = k_scale * q_factor;
+        float f = k_scale * q_factor;
         uint32_t seen[2] = {~0u, ~0u};  // a bit per key of mine
         if (masked) {
             const int low = p.a.window > 0 ? pos - p.a.window : -1;
@@ -274,12 +273,19 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         if (__builtin_amdgcn_ballot_w64(move) != 0 || by_e != 1.f) {
             const float ref = move ? fmaxf(mx, kLowestRef) - kRefLead : st.ref;
             const float alpha = move ? __builtin_amdgcn_exp2f(st.ref - ref) : 1.f;
-            far = far || (move && fabsf(ref) > kFarScore);  // a score above the reference's lead moves it
             st.ref = ref;
             st.sum *= alpha;
             rescale(alpha * by_e);
         }
-        const float off = mant - st.ref;
+        float off = mant - st.ref;
+        if (__builtin_amdgcn_ballot_w64(fabsf(mx) > kFarScore) != 0) {  // see above
+#pragma unroll
+            for (int j = 0; j < 2; j++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) s[j][i] = s[j][i] * f - st.ref;
+            f = 1.f;
+            off = mant;
+        }
         float sum = 0.f;
         const half2v ones = {(_Float16)1.f, (_Float16)1.f};
 #pragma unroll
@@ -496,11 +502,9 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         sum = __uint_as_float(both[0]) + __uint_as_float(both[1]);
     }
     e_ref = max(e_ref, -140);  // still there where nothing was met
-    const bool refused = rt.bad || far;
-    if (live && far) flag(p.g.fault, kFaultScore);
     if (p.splits == 1) {
         if (!live) return;
-        const float f = refused ? __builtin_nanf("") : sum == 0.f ? 0.f : 1.f / sum, unit_v = ldexpf(1.f, e_ref);
+        const float f = rt.bad ? __builtin_nanf("") : sum == 0.f ? 0.f : 1.f / sum, unit_v = ldexpf(1.f, e_ref);
 #pragma unroll
         for (int c = 0; c < D / 32; c++) st.o[c] *= f;  // first: with their unit they could be too large
         store_rows<T, D>(p.a.out + (size_t)(rt.start + place) * p.a.out_stride + (size_t)head * D, half, st, unit_v);
@@ -516,7 +520,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
                 make_float4(st.o[c][i], st.o[c][i + 1], st.o[c][i + 2], st.o[c][i + 3]);
     if (half == 0) {
         part[D] = st.ref;
-        part[D + 1] = refused ? __builtin_nanf("") : sum;
+        part[D + 1] = rt.bad ? __builtin_nanf("") : sum;
         part[D + 2] = (float)e_ref;
     }
 }

@@ -638,13 +638,9 @@ def test_attention_at_the_ends_of_the_range_of_bf16(gpu):
     q = w.rand(6, 2, 64).to(torch.bfloat16)
     got = w.cache.attn_decode(q.cuda(), 0.125, _i32(w.lens), w.d_table, w.d_tails, q_len=3)
     _close(got, *_reference(w, [3, 3], 0, 0.125, q), w.dtype)
-    w.cache.check()
     got = w.cache.attn_prefill(q.cuda(), 0.125, _starts([3, 3]), _i32(w.lens), w.d_table, w.d_tails)
-    assert torch.isnan(got).all()  # refused, and said so
-    with pytest.raises(gpu.KvcompError) as e:
-        w.cache.check()
-    assert e.value.status == gpu.ERR_STATE
-    # scores up to 2^25 are taken (an error of theirs is a common factor of a row's weights, or lies within `spread`)
+    _close_chunks(got, *_reference(w, [3, 3], 0, 0.125, q), w.dtype)
+    # scores around 2^25: an error of theirs is a common factor of a row's weights, or lies within `spread`
     w = World(gpu, 2, 1, 2, 64, torch.bfloat16, "e4m3", 3, seed=3)
     k, v, _ = w.tokens(2 * 150)
     k = (k.double() * 1e5).to(torch.bfloat16)
