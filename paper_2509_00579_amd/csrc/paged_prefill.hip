@@ -160,7 +160,6 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
     constexpr int kPreWaves = W, kPreRows = 32 * W, kPreThreads = 64 * W;
     constexpr int kUnits = kPBT * D / 8, kPieces = (kPBT * D / 16 + kPreThreads - 1) / kPreThreads;  // 16-byte units of a tile; pieces of 16 codes per thread
     extern __shared__ __align__(16) uint4 s_tiles[];  // [2 buffers][K, V][kUnits]
-    __shared__ uint32_t s_big[2][kPreWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n = lane & 31, half = lane >> 5;
     const int h = uniform(blockIdx.x % p.g.H), rest = uniform(blockIdx.x / p.g.H), split = uniform(rest % p.splits), unit = p.units - 1 - uniform(rest / p.splits);
     const RowTile rt = find_tile(p, unit, lane);
@@ -177,17 +176,25 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
     const int t0 = uniform(from + (int)((long long)blocks * split / p.splits)), t1 = uniform(from + (int)((long long)blocks * (split + 1) / p.splits));
 
     constexpr int KS = D / 16;
+    // Page numbers first, then the queries: what hangs on the former is asked for while the latter come.
+    const int32_t *pages = p.g.table + (size_t)rt.b * p.g.max_pages;
+    const int unfinished = rt.len / kPBT;  // this block is in 16 bits
+    const int t_pages = min(t1, unfinished);
+    auto page_of = [&](int t) { return t + lane < t_pages ? pages[t + lane] : 0; };
+    const int first_pages = page_of(t0);
     half8v qf[KS];
     float q_factor = fabsf(p.a.scale);
+    uint4 qw[KS];
     {
         const uint16_t *q = p.a.q + (size_t)(rt.start + place) * p.a.q_stride + (size_t)head * D + 8 * half;
+#pragma unroll
+        for (int k = 0; k < KS; k++) qw[k] = live ? *reinterpret_cast<const uint4 *>(q + 16 * k) : make_uint4(0, 0, 0, 0);
+    }
+    auto ready_queries = [&]() __attribute__((always_inline)) {
         const uint32_t turn = p.a.scale < 0.f ? 0x80008000u : 0u;
         uint4 w[KS];
 #pragma unroll
-        for (int k = 0; k < KS; k++) {
-            w[k] = live ? *reinterpret_cast<const uint4 *>(q + 16 * k) : make_uint4(0, 0, 0, 0);
-            w[k] = make_uint4(w[k].x ^ turn, w[k].y ^ turn, w[k].z ^ turn, w[k].w ^ turn);
-        }
+        for (int k = 0; k < KS; k++) w[k] = make_uint4(qw[k].x ^ turn, qw[k].y ^ turn, qw[k].z ^ turn, qw[k].w ^ turn);
         if constexpr (T == kBF16) {
             uint32_t big = 0;
 #pragma unroll
@@ -202,7 +209,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         }
 #pragma unroll
         for (int k = 0; k < KS; k++) qf[k] = __builtin_bit_cast(half8v, w[k]);
-    }
+    };
     RowState<D> st;
 #pragma unroll
     for (int c = 0; c < D / 32; c++)
@@ -323,27 +330,23 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
     };
 
     // Page numbers and scales of 64 blocks, a block a lane; V's as its exponent, log2 of its mantissa and what takes that out again.
-    const int32_t *pages = p.g.table + (size_t)rt.b * p.g.max_pages;
-    const int unfinished = rt.len / kPBT;  // this block is in 16 bits
-    const int t_pages = min(t1, unfinished);
     int known = t0, known_page = 0, known_e = -127;
     float known_k = 0.f, known_mant = 0.f, known_inv = 1.f;
-    auto learn = [&](int t) __attribute__((always_inline)) {
+    auto learn_pages = [&](int t, int page) __attribute__((always_inline)) {
         known = t;
-        if (t + lane < t_pages) {
-            known_page = pages[t + lane];
-            const bool ok = (unsigned)known_page < (unsigned)p.g.n_pages;
-            if (!ok) {
-                flag(p.g.fault, kFaultPage);
-                known_page = 0;
-            }
-            const float2 sc = *reinterpret_cast<const float2 *>(p.g.scales + ((size_t)known_page * p.g.H + h) * 2);
-            known_k = ok ? sc.x : __builtin_nanf("");
-            const bool any = sc.y > 0.f;
-            known_e = any ? ilogbf(sc.y) : -127;
-            known_mant = any ? __builtin_amdgcn_logf(ldexpf(sc.y, -known_e)) : 0.f;
-            known_inv = __builtin_amdgcn_exp2f(-known_mant);
-        }
+        const bool ok = (unsigned)page < (unsigned)p.g.n_pages;
+        if (!ok) flag(p.g.fault, kFaultPage);
+        known_page = ok ? page : 0;
+        float2 sc = *reinterpret_cast<const float2 *>(p.g.scales + ((size_t)known_page * p.g.H + h) * 2);
+        if (!ok) sc.x = __builtin_nanf("");
+        return sc;
+    };
+    auto learn_scales = [&](float2 sc) __attribute__((always_inline)) {
+        known_k = sc.x;
+        const bool any = sc.y > 0.f;
+        known_e = any ? ilogbf(sc.y) : -127;
+        known_mant = any ? __builtin_amdgcn_logf(ldexpf(sc.y, -known_e)) : 0.f;
+        known_inv = __builtin_amdgcn_exp2f(-known_mant);
     };
     auto e_of = [&](int t) { return __builtin_amdgcn_readlane(known_e, t - known); };
     auto power_of_2 = [&](int e) { return __uint_as_float((uint32_t)max(e + 127, 0) << 23); };  // 0 below the normal range
@@ -359,12 +362,12 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
     int e_staged = -10000;
     // Behind the last block the same is done with it again, into buffers that nobody will read: a branch around it would cost the
     // loop copies of whatever it leaves in registers.
-    auto fetch_k = [&](int t) __attribute__((always_inline)) {
+    auto fetch_k = [&](int t, uint4 (&c)[kPieces]) __attribute__((always_inline)) {
         t = min(t, t_pages - 1);
         const uint4 *k = reinterpret_cast<const uint4 *>(p.g.k_codes + ((size_t)__builtin_amdgcn_readlane(known_page, t - known) * p.g.H + h) * kPBT * D);
 #pragma unroll
         for (int i = 0; i < kPieces; i++)
-            if (k_piece + i * kPreThreads < kTilePieces) ck[i] = k[k_piece + i * kPreThreads];
+            if (k_piece + i * kPreThreads < kTilePieces) c[i] = k[k_piece + i * kPreThreads];
     };
     auto fetch_v = [&](int t) __attribute__((always_inline)) {
         t = min(t, t_pages - 1);
@@ -373,13 +376,13 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         for (int i = 0; i < kPieces; i++)
             if (v_piece + i * kPreThreads < kTilePieces) cv[i] = v[v_piece + i * kPreThreads];
     };
-    auto stage_k = [&](uint4 *sk) __attribute__((always_inline)) {
+    auto stage_k = [&](uint4 *sk, const uint4 (&c)[kPieces]) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < kPieces; i++) {
             const int piece = k_piece + i * kPreThreads, token = piece / (D / 16), chunk = piece % (D / 16) * 2;
             if (piece >= kTilePieces) break;
-            sk[k_unit<D>(token, chunk)] = widen8_by<C>(ck[i].x, ck[i].y, 1.f);
-            sk[k_unit<D>(token, chunk + 1)] = widen8_by<C>(ck[i].z, ck[i].w, 1.f);
+            sk[k_unit<D>(token, chunk)] = widen8_by<C>(c[i].x, c[i].y, 1.f);
+            sk[k_unit<D>(token, chunk + 1)] = widen8_by<C>(c[i].z, c[i].w, 1.f);
         }
     };
     auto stage_v = [&](int t, uint4 *sv) __attribute__((always_inline)) {
@@ -396,30 +399,33 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
     };
     if (t0 < t_pages) {
         auto buffer = [&](int t) { return s_tiles + ((t - t0) & 1) * 2 * kUnits; };
-        learn(t0);
-        fetch_k(t0);
-        stage_k(s_tiles);
+        uint4 c0[kPieces];
+        const float2 first_scales = learn_pages(t0, first_pages);
+        fetch_k(t0, c0);
+        fetch_k(t0 + 1, ck);
+        fetch_v(t0);
+        learn_scales(first_scales);
+        ready_queries();
+        stage_k(s_tiles, c0);
         if (lead) {
-            fetch_k(t0 + 1);
-            fetch_v(t0);
-            stage_k(s_tiles + 2 * kUnits);
+            stage_k(s_tiles + 2 * kUnits, ck);
             stage_v(t0, s_tiles + kUnits);
+            fetch_k(t0 + 2, ck);
+            fetch_v(t0 + 1);
         }
-        fetch_k(t0 + 1 + lead);
-        fetch_v(t0 + lead);
         lds_barrier();
         scores(0);
         if (lead) lds_barrier();
         for (int t = t0; t < t_pages; t++) {
-            if (t + 4 > known + 64) learn(t);
+            if (t + 4 > known + 64) learn_scales(learn_pages(t, page_of(t)));
             const int mine = (t - t0) & 1;
             const int e = e_of(t);
             const float by_e = to_larger(e);
             e_ref = max(e, e_ref);
             weigh(t, bcast(known_k, t - known), bcast(known_mant, t - known), bcast(known_inv, t - known), by_e, some_hidden(t));
-            stage_k(buffer(t + 1 + lead));
+            stage_k(buffer(t + 1 + lead), ck);
             stage_v(t + lead, buffer(t + lead) + kUnits);
-            fetch_k(t + 2 + lead);
+            fetch_k(t + 2 + lead, ck);
             fetch_v(t + 1 + lead);
             lds_barrier();
             __builtin_amdgcn_s_setprio(1);
@@ -429,71 +435,86 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
             if (kGroups == 2) lds_barrier();
         }
         if (kGroups == 2 && !lead) lds_barrier();
+    } else {
+        ready_queries();
     }
     if (t_pages < t1) {
-        // the block that is still in 16 bits: K as it is (bf16: times a power of two), V turned and brought to the accumulators' unit
+        // The block that is still in 16 bits, on products of its own type: K as it is, V turned.  fp16: V counts as scaled by one; bf16: the
+        // accumulators change to a unit that no sum of its values overflows, and the weights are taken to it in two parts.
         const int t = unfinished, count = rt.len - t * kPBT;
         uint4 *sk = s_tiles, *sv = sk + kUnits;
         const size_t at = ((size_t)rt.tail * p.g.H + h) * kPBT * D;
         constexpr int kRowUnits = D / 8, kMine = kUnits / kPreThreads;
-        uint32_t bk = 0, bv = 0;
-        auto largest = [](uint32_t m, uint4 v) {
-#pragma unroll
-            for (int c = 0; c < 4; c++) {
-                const uint32_t w = c == 0 ? v.x : c == 1 ? v.y : c == 2 ? v.z : v.w, lo = w & 0x7fffu, hi = (w >> 16) & 0x7fffu;
-                m = lo < kInfBits<T> && lo > m ? lo : m;
-                m = hi < kInfBits<T> && hi > m ? hi : m;
-            }
-            return m;
-        };
         const uint4 *tk = reinterpret_cast<const uint4 *>(p.g.k_tail + at), *tv = reinterpret_cast<const uint4 *>(p.g.v_tail + at);
+        uint4 rk[kMine], rv[kMine];
 #pragma unroll
         for (int i = 0; i < kMine; i++) {
             const int u = tid + i * kPreThreads;
-            if (u / kRowUnits >= count) break;
-            if (T == kBF16) bk = largest(bk, tk[u]);
-            bv = largest(bv, tv[u]);
+            const bool in = u / kRowUnits < count;
+            rk[i] = in ? tk[u] : make_uint4(0, 0, 0, 0);
+            rv[i] = in ? tv[u] : make_uint4(0, 0, 0, 0);
         }
-        for (int x = 1; x < 64; x <<= 1) {
-            bk = max(bk, (uint32_t)__shfl_xor((int)bk, x));
-            bv = max(bv, (uint32_t)__shfl_xor((int)bv, x));
-        }
-        if (lane == 0) {
-            s_big[0][wave] = bk;
-            s_big[1][wave] = bv;
-        }
-        __syncthreads();
-        for (int i = 0; i < kPreWaves; i++) {
-            bk = max(bk, s_big[0][i]);
-            bv = max(bv, s_big[1][i]);
-        }
-        // the largest V to 2^14 .. 2^15; in fp16 the exponent of subnormal magnitudes counts as the smallest normal one
-        const int shift_k = T == kBF16 ? bf16_shift(uniform(bk)) : 0;
-        const int shift_v = T == kBF16 ? bf16_shift(uniform(bv)) : 29 - (int)max((uint32_t)uniform(bv) >> 10, 1u);
-        const int e = -shift_v, top = max(e, e_ref);
+        const int e = T == kBF16 ? 24 : 0;
         const float by_e = to_larger(e);
-        e_ref = top;
-        for (int u = tid; u < kUnits; u += kPreThreads) {
-            const int row = u / kRowUnits, chunk = u % kRowUnits;
-            uint4 x = make_uint4(0, 0, 0, 0), y = x;
-            if (row < count) {
-                x = tk[u];
-                y = tv[u];
-            }
-            if constexpr (T == kBF16)
-                x = make_uint4(bf16_to_half2(x.x, shift_k), bf16_to_half2(x.y, shift_k), bf16_to_half2(x.z, shift_k), bf16_to_half2(x.w, shift_k));
-            sk[k_unit<D>(row, chunk)] = x;
-            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+        e_ref = max(e, e_ref);
+        const float v_by = T == kBF16 ? 1.f : power_of_2(-e_ref), w_by = T == kBF16 ? power_of_2(-e_ref) : 1.f;
+        __syncthreads();  // the tiles are free
+#pragma unroll
+        for (int i = 0; i < kMine; i++) {
+            const int u = tid + i * kPreThreads, row = u / kRowUnits, chunk = u % kRowUnits;
+            sk[k_unit<D>(row, chunk)] = rk[i];
+            const uint32_t w[4] = {rv[i].x, rv[i].y, rv[i].z, rv[i].w};
 #pragma unroll
             for (int c = 0; c < 8; c++) {
-                const float v = c & 1 ? wide_hi<T>(w[c >> 1]) : wide_lo<T>(w[c >> 1]);
-                reinterpret_cast<_Float16 *>(sv + v_unit(8 * chunk + c, row >> 3))[row & 7] = (_Float16)ldexpf(v, -top);
+                const uint32_t x = c & 1 ? w[c >> 1] >> 16 : w[c >> 1] & 0xffffu;
+                uint16_t *to = reinterpret_cast<uint16_t *>(sv + v_unit(8 * chunk + c, row >> 3)) + (row & 7);
+                if constexpr (T == kBF16) *to = (uint16_t)x;
+                else *to = __builtin_bit_cast(uint16_t, (_Float16)((float)__builtin_bit_cast(_Float16, (uint16_t)x) * v_by));
             }
         }
         __syncthreads();
-        scores(0);
-        weigh(t, ldexpf(1.f, -shift_k), 0.f, 1.f, by_e, true);
-        add_values(0);
+        if constexpr (T == kF16) {
+            scores(0);
+            weigh(t, 1.f, 0.f, 1.f, by_e, true);
+            add_values(0);
+        } else {
+            constexpr float kBack = 6.103515625e-05f;  // 2^-14: the queries' largest between 1 and 2, exactly
+            typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+#pragma unroll
+            for (int j = 0; j < 2; j++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) s[j][i] = 0.f;
+#pragma unroll
+            for (int k = 0; k < KS; k++) {
+                uint32_t w[4];
+#pragma unroll
+                for (int x = 0; x < 4; x++) w[x] = narrow2<kBF16>((float)qf[k][2 * x] * kBack, (float)qf[k][2 * x + 1] * kBack);
+                const bf8 q = __builtin_bit_cast(bf8, make_uint4(w[0], w[1], w[2], w[3]));
+#pragma unroll
+                for (int j = 0; j < 2; j++)
+                    s[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        *reinterpret_cast<const bf8 *>(tiles + (k_first ^ (k << 5)) + j * 32 * D * 2), q, s[j], 0, 0, 0);
+            }
+            weigh(t, 1.f / kBack, 0.f, 1.f, by_e, true);
+#pragma unroll
+            for (int part = 0; part < 2; part++)
+#pragma unroll
+                for (int x = 0; x < 4; x++) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {  // a weight's 11 bits are two times 8
+                        const uint32_t both = pw[x >> 1][4 * (x & 1) + i];
+                        const float a = wide_lo<kF16>(both) * w_by, b = wide_hi<kF16>(both) * w_by;
+                        w[i] = narrow2<kBF16>(a, b);
+                        if (part) w[i] = narrow2<kBF16>(a - wide_lo<kBF16>(w[i]), b - wide_hi<kBF16>(w[i]));
+                    }
+                    const bf8 pf = __builtin_bit_cast(bf8, make_uint4(w[0], w[1], w[2], w[3]));
+#pragma unroll
+                    for (int c = 0; c < D / 32; c++)
+                        st.o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            *reinterpret_cast<const bf8 *>(tiles + ((v_first + kUnits * 16) ^ (x << 5)) + c * 32 * kPBT * 2), pf, st.o[c], 0, 0, 0);
+                }
+        }
     }
 
     float sum;
