@@ -143,11 +143,31 @@ __device__ __forceinline__ uint32_t bf16_to_half2(uint32_t w, int shift) {
     const half2v v = {(_Float16)ldexpf(wide_lo<kBF16>(w), shift), (_Float16)ldexpf(wide_hi<kBF16>(w), shift)};
     return __builtin_bit_cast(uint32_t, v);
 }
-// The largest finite magnitude among the two values of a word and `m` (a bit pattern).
-__device__ __forceinline__ uint32_t bf16_largest(uint32_t m, uint32_t w) {
-    const uint32_t lo = w & 0x7fffu, hi = (w >> 16) & 0x7fffu;
-    m = lo < 0x7f80u && lo > m ? lo : m;
-    return hi < 0x7f80u && hi > m ? hi : m;
+// Both halves of two words compared as unsigned numbers; 16-bit magnitudes are ordered like the values they stand for.
+__device__ __forceinline__ uint32_t max16(uint32_t a, uint32_t b) {
+    typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, a), __builtin_bit_cast(us2, b)));
+}
+// The largest finite magnitude (a bit pattern) among `count` times eight bf16 values.
+template <int count>
+__device__ __forceinline__ uint32_t bf16_largest(const uint4 (&w)[count]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < count; k++)
+        m = max16(max16(max16(max16(m, w[k].x & 0x7fff7fffu), w[k].y & 0x7fff7fffu), w[k].z & 0x7fff7fffu), w[k].w & 0x7fff7fffu);
+    m = max(m & 0xffffu, m >> 16);
+    if (m >= 0x7f80u) {  // Inf or NaN: leave them out
+        m = 0;
+#pragma unroll
+        for (int k = 0; k < count; k++)
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                const uint32_t x = c == 0 ? w[k].x : c == 1 ? w[k].y : c == 2 ? w[k].z : w[k].w, lo = x & 0x7fffu, hi = (x >> 16) & 0x7fffu;
+                m = lo < 0x7f80u && lo > m ? lo : m;
+                m = hi < 0x7f80u && hi > m ? hi : m;
+            }
+    }
+    return m;
 }
 
 // Across the four groups of 16 lanes of a wave, and across its halves.

@@ -87,11 +87,6 @@ __device__ __forceinline__ void stream16(uint16_t *p, const uint32_t (&w)[4]) {
     const u4 v = {w[0], w[1], w[2], w[3]};
     __builtin_nontemporal_store(v, reinterpret_cast<u4 *>(p));
 }
-__device__ __forceinline__ uint32_t max16(uint32_t a, uint32_t b) {  // both halves, unsigned
-    typedef unsigned short us2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, a), __builtin_bit_cast(us2, b)));
-}
-
 // Values that are Inf or NaN: zero in V, and a NaN in the same token's K marks the token for whoever reads it.
 template <int T>
 __device__ __forceinline__ bool poison(uint32_t (&k)[2][4], uint32_t (&v)[2][4]) {

@@ -108,9 +108,7 @@ struct Wave {
             for (int k = 0; k < KS; k++) w[k] = qw[r][k];
             q_factor[r] = 1.f;
             if constexpr (T == kBF16) {
-                uint32_t big = 0;
-#pragma unroll
-                for (int k = 0; k < KS; k++) big = bf16_largest(bf16_largest(bf16_largest(bf16_largest(big, w[k].x), w[k].y), w[k].z), w[k].w);
+                uint32_t big = bf16_largest(w);
                 big = max_rows_u(big);
                 const int shift = bf16_shift(big);
                 q_factor[r] = ldexpf(1.f, -shift);

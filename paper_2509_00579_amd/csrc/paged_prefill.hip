@@ -196,9 +196,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
 #pragma unroll
         for (int k = 0; k < KS; k++) w[k] = make_uint4(qw[k].x ^ turn, qw[k].y ^ turn, qw[k].z ^ turn, qw[k].w ^ turn);
         if constexpr (T == kBF16) {
-            uint32_t big = 0;
-#pragma unroll
-            for (int k = 0; k < KS; k++) big = bf16_largest(bf16_largest(bf16_largest(bf16_largest(big, w[k].x), w[k].y), w[k].z), w[k].w);
+            const uint32_t big = bf16_largest(w);
             const auto both = __builtin_amdgcn_permlane32_swap(big, big, false, false);
             const int shift = bf16_shift(max(both[0], both[1]));
             q_factor = ldexpf(q_factor, -shift);
@@ -397,6 +395,21 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
             sv[v_unit(channel, part + 1)] = widen8_by<C>(cv[i].z, cv[i].w, by);
         }
     };
+    // The unfinished block's rows, asked for before the others where there are registers to hold them.
+    constexpr bool kTailAhead = D == 128;
+    constexpr int kRowUnits = D / 8, kMine = kUnits / kPreThreads;
+    uint4 rk[kMine], rv[kMine];
+    auto ask_tail = [&]() __attribute__((always_inline)) {
+        const size_t at = ((size_t)rt.tail * p.g.H + h) * kPBT * D;
+        const uint4 *tk = reinterpret_cast<const uint4 *>(p.g.k_tail + at), *tv = reinterpret_cast<const uint4 *>(p.g.v_tail + at);
+#pragma unroll
+        for (int i = 0; i < kMine; i++) {
+            const int u = tid + i * kPreThreads;
+            const bool in = u / kRowUnits < rt.len - unfinished * kPBT;
+            rk[i] = in ? tk[u] : make_uint4(0, 0, 0, 0);
+            rv[i] = in ? tv[u] : make_uint4(0, 0, 0, 0);
+        }
+    };
     if (t0 < t_pages) {
         auto buffer = [&](int t) { return s_tiles + ((t - t0) & 1) * 2 * kUnits; };
         uint4 c0[kPieces];
@@ -413,6 +426,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
             fetch_k(t0 + 2, ck);
             fetch_v(t0 + 1);
         }
+        if (kTailAhead && t_pages < t1) ask_tail();
         lds_barrier();
         scores(0);
         if (lead) lds_barrier();
@@ -436,24 +450,15 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         }
         if (kGroups == 2 && !lead) lds_barrier();
     } else {
+        if (kTailAhead && t_pages < t1) ask_tail();
         ready_queries();
     }
     if (t_pages < t1) {
         // The block that is still in 16 bits, on products of its own type: K as it is, V turned.  fp16: V counts as scaled by one; bf16: the
         // accumulators change to a unit that no sum of its values overflows, and the weights are taken to it in two parts.
-        const int t = unfinished, count = rt.len - t * kPBT;
+        const int t = unfinished;
         uint4 *sk = s_tiles, *sv = sk + kUnits;
-        const size_t at = ((size_t)rt.tail * p.g.H + h) * kPBT * D;
-        constexpr int kRowUnits = D / 8, kMine = kUnits / kPreThreads;
-        const uint4 *tk = reinterpret_cast<const uint4 *>(p.g.k_tail + at), *tv = reinterpret_cast<const uint4 *>(p.g.v_tail + at);
-        uint4 rk[kMine], rv[kMine];
-#pragma unroll
-        for (int i = 0; i < kMine; i++) {
-            const int u = tid + i * kPreThreads;
-            const bool in = u / kRowUnits < count;
-            rk[i] = in ? tk[u] : make_uint4(0, 0, 0, 0);
-            rv[i] = in ? tv[u] : make_uint4(0, 0, 0, 0);
-        }
+        if (!kTailAhead) ask_tail();
         const int e = T == kBF16 ? 24 : 0;
         const float by_e = to_larger(e);
         e_ref = max(e, e_ref);
@@ -628,7 +633,9 @@ hipError_t launch_tiles(PrefillArgs p, int max_len, hipStream_t s) {
 
 template <int T, int C, int D>
 hipError_t launch(const PrefillArgs &p, int max_new, int max_len, hipStream_t s) {
-    if (D == 128 && (max_new == 0 || (long long)max_new * p.g.G > 128)) return launch_tiles<T, C, D, 8>(p, max_len, s);
+    if constexpr (D == 128) {
+        if (max_new == 0 || (long long)max_new * p.g.G > 128) return launch_tiles<T, C, D, 8>(p, max_len, s);
+    }
     return launch_tiles<T, C, D, 4>(p, max_len, s);
 }
 
