@@ -305,7 +305,7 @@ typedef struct {        /* the new tokens of one append                         
     const void *d_k, *d_v;       /* DEVICE [n_tokens][n_kv_heads][head_dim], 16-byte aligned                    */
     size_t k_stride, v_stride;   /* elements between tokens, multiples of 8                                     */
     const void *d_q;             /* DEVICE [n_tokens][n_q_heads][head_dim]: queries to rotate along, or NULL    */
-    void *d_q_out;               /* may be d_q (then with its stride)                                           */
+    void *d_q_out;               /* may be d_q (then with its stride); overlaps d_q, d_k and d_v nowhere else    */
     size_t q_stride, q_out_stride;
     const float *d_cos_sin;      /* DEVICE fp32 [n_positions][rot_dim]: cosines of the rot_dim / 2 pairs, then their sines;
                                     NULL: no rotation */
@@ -332,8 +332,9 @@ size_t kvcomp_paged_workspace_bytes(const kvcomp_paged_config *cfg);
  * sequence b is d_q row b * q_len + i, stands at position lens[b] - q_len + i and sees the keys at positions up to its own
  * and, with window > 0, above its own minus window.  out = softmax(scale * q.K^T) . V over those, sums in binary32, one
  * rounding to the 16-bit type; a row that sees nothing is zero.  d_q, d_out: DEVICE [batch * q_len][n_q_heads][head_dim],
- * 16-byte aligned, strides in elements between rows, multiples of 8.  max_len: the longest length as far as the caller
- * knows (0: max_pages * 64); it sizes the launch only.  batch <= 4096.
+ * 16-byte aligned, strides in elements between rows, multiples of 8; the two have no row in common (but may be slices of
+ * one buffer's rows).  max_len: the longest length as far as the caller knows (0: max_pages * 64); it sizes the launch only.
+ * batch <= 4096.
  * Errors: INVALID_ARG, CAPACITY (workspace too small), HIP. */
 kvcomp_status kvcomp_paged_attn_decode(const kvcomp_paged_config *cfg, const kvcomp_paged_cache *cache,
                                        const kvcomp_paged_batch *seqs, const void *d_q, size_t q_stride, int q_len, float scale,
@@ -342,7 +343,7 @@ kvcomp_status kvcomp_paged_attn_decode(const kvcomp_paged_config *cfg, const kvc
 
 /* Attention of chunks of new tokens: rows starts[b] .. starts[b+1]-1 of d_q (d_starts: DEVICE int32 [batch + 1]) are the last
  * tokens of sequence b, row starts[b] + i stands at position lens[b] - (starts[b+1] - starts[b]) + i and sees what a decode
- * row at that position sees.  d_q, d_out: DEVICE [n_tokens][n_q_heads][head_dim]; rows of d_out outside every sequence's
+ * row at that position sees.  d_q, d_out: DEVICE [n_tokens][n_q_heads][head_dim], as above; rows of d_out outside every sequence's
  * range, and those of a sequence whose starts do not fit into n_tokens, are left as they were.  max_new, max_len: the most new
  * tokens and the longest length as far as the caller knows (0: no idea); they shape the launch only.  One kernel, and a
  * second one where few rows over long sequences make it split the keys.  Errors: INVALID_ARG, CAPACITY, HIP. */

@@ -472,6 +472,8 @@ class PagedCache:
         axes, sections = 1, (0, 0, 0)
         if starts is not None:
             sp = self._starts(starts, batch)
+        assert q is not None or q_out is None, "q_out without q"
+        assert rope is not None or positions is None, "positions without rope"
         if q is not None:
             if q_out is None:
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)

@@ -59,6 +59,15 @@ kvcomp_status check_rows(const char *name, const void *p, size_t stride, int hea
     return KVCOMP_OK;
 }
 
+// Whether two tensors of `rows` rows have 16-bit elements in common; slices of one buffer's rows do not.
+bool overlap(const void *a, size_t a_stride, size_t a_width, const void *b, size_t b_stride, size_t b_width, long long rows) {
+    if (reinterpret_cast<uintptr_t>(a) > reinterpret_cast<uintptr_t>(b)) return overlap(b, b_stride, b_width, a, a_stride, a_width, rows);
+    const size_t off = (reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a)) / 2;
+    if (off >= (size_t)(rows - 1) * a_stride + a_width) return false;
+    if (rows == 1 || a_stride != b_stride) return true;
+    return off % a_stride < a_width || off % a_stride + b_width > a_stride;
+}
+
 }  // namespace
 
 extern "C" {
@@ -101,7 +110,12 @@ kvcomp_status kvcomp_paged_append(const kvcomp_paged_config *cfg, const kvcomp_p
     if (f.d_q || f.d_q_out) {
         if ((st = check_rows("d_q", f.d_q, f.q_stride, cfg->n_q_heads, cfg->head_dim))) return st;
         if ((st = check_rows("d_q_out", f.d_q_out, f.q_out_stride, cfg->n_q_heads, cfg->head_dim))) return st;
-        if (f.d_q == f.d_q_out && f.q_stride != f.q_out_stride) return fail(KVCOMP_ERR_INVALID_ARG, "queries in place with another stride");
+        const size_t wq = (size_t)cfg->n_q_heads * cfg->head_dim, wk = (size_t)cfg->n_kv_heads * cfg->head_dim;
+        const bool in_place = f.d_q == f.d_q_out && f.q_stride == f.q_out_stride;
+        if ((!in_place && overlap(f.d_q, f.q_stride, wq, f.d_q_out, f.q_out_stride, wq, f.n_tokens)) ||
+            overlap(f.d_k, f.k_stride, wk, f.d_q_out, f.q_out_stride, wq, f.n_tokens) ||
+            overlap(f.d_v, f.v_stride, wk, f.d_q_out, f.q_out_stride, wq, f.n_tokens))
+            return fail(KVCOMP_ERR_INVALID_ARG, "d_q_out overlaps d_q (and is not the same rows), d_k or d_v");
     }
     n.n_tokens = f.n_tokens;
     n.starts = f.d_starts;
@@ -124,20 +138,23 @@ size_t kvcomp_paged_workspace_bytes(const kvcomp_paged_config *cfg) {
 }
 
 // what both attention calls are given; sets up `a`
-static kvcomp_status check_attn(const kvcomp_paged_config *cfg, const void *d_q, size_t q_stride, float scale, int window, void *d_out,
+static kvcomp_status check_attn(const kvcomp_paged_config *cfg, long long rows, const void *d_q, size_t q_stride, float scale, int window, void *d_out,
                                 size_t out_stride, void *d_workspace, size_t workspace_bytes, PagedAttn *a) {
     kvcomp_status st;
     if ((st = check_rows("d_q", d_q, q_stride, cfg->n_q_heads, cfg->head_dim))) return st;
     if ((st = check_rows("d_out", d_out, out_stride, cfg->n_q_heads, cfg->head_dim))) return st;
+    const size_t width = (size_t)cfg->n_q_heads * cfg->head_dim;
+    if (overlap(d_q, q_stride, width, d_out, out_stride, width, rows)) return fail(KVCOMP_ERR_INVALID_ARG, "d_q and d_out overlap");
     if (!d_workspace || !aligned16(d_workspace)) return fail(KVCOMP_ERR_INVALID_ARG, "the workspace must be 16-byte aligned");
     if (workspace_bytes < kvcomp_paged_workspace_bytes(cfg)) return fail(KVCOMP_ERR_CAPACITY, "workspace too small");
-    if (!(scale - scale == 0.f)) return fail(KVCOMP_ERR_INVALID_ARG, "scale must be finite");
+    const float scale2 = scale * 1.44269504088896f;  // to powers of two
+    if (!(scale2 - scale2 == 0.f)) return fail(KVCOMP_ERR_INVALID_ARG, "scale times log2(e) must be finite");
     if (window < 0) return fail(KVCOMP_ERR_INVALID_ARG, "window is negative");
     a->q = static_cast<const uint16_t *>(d_q);
     a->out = static_cast<uint16_t *>(d_out);
     a->q_stride = q_stride;
     a->out_stride = out_stride;
-    a->scale = scale * 1.44269504088896f;
+    a->scale = scale2;
     a->window = window > kMaxPagesPerSeq * kPBT ? 0 : window;
     a->tickets = static_cast<uint32_t *>(d_workspace);
     a->partials = static_cast<float *>(d_workspace) + kTicketWords;
@@ -159,7 +176,7 @@ kvcomp_status kvcomp_paged_attn_decode(const kvcomp_paged_config *cfg, const kvc
         return fail(KVCOMP_ERR_INVALID_ARG, "more than 2^31 - 1 sequences times KV heads times max_pages");
     if (max_len < 0) return fail(KVCOMP_ERR_INVALID_ARG, "max_len is negative");
     if (!g.batch) return KVCOMP_OK;
-    if ((st = check_attn(cfg, d_q, q_stride, scale, window, d_out, out_stride, d_workspace, workspace_bytes, &a))) return st;
+    if ((st = check_attn(cfg, (long long)g.batch * q_len, d_q, q_stride, scale, window, d_out, out_stride, d_workspace, workspace_bytes, &a))) return st;
     HIP_TRY(launch_paged_decode(g, a, q_len, max_len, cfg->head_dim, cfg->data_type, cfg->code_type, static_cast<hipStream_t>(stream)));
     return KVCOMP_OK;
 }
@@ -176,7 +193,7 @@ kvcomp_status kvcomp_paged_attn_prefill(const kvcomp_paged_config *cfg, const kv
     if (n_tokens < 0 || max_new < 0 || max_len < 0) return fail(KVCOMP_ERR_INVALID_ARG, "n_tokens, max_new or max_len is negative");
     if ((long long)n_tokens * cfg->n_q_heads > (1ll << 30)) return fail(KVCOMP_ERR_INVALID_ARG, "more than 2^30 tokens times query heads");
     if (!g.batch || !n_tokens) return KVCOMP_OK;
-    if ((st = check_attn(cfg, d_q, q_stride, scale, window, d_out, out_stride, d_workspace, workspace_bytes, &a))) return st;
+    if ((st = check_attn(cfg, n_tokens, d_q, q_stride, scale, window, d_out, out_stride, d_workspace, workspace_bytes, &a))) return st;
     HIP_TRY(launch_paged_prefill(g, a, static_cast<const int32_t *>(d_starts), n_tokens, max_new, max_len, cfg->head_dim,
                                  cfg->data_type, cfg->code_type, static_cast<hipStream_t>(stream)));
     return KVCOMP_OK;

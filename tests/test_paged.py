@@ -768,3 +768,73 @@ def test_a_prompt_a_chunk_and_steps_as_a_server_runs_them(gpu):
             del x[-2:]
     chunk([3, 100, 60])
     w.check()
+
+
+def test_prefill_captured_on_another_stream_and_replayed_with_other_lengths(gpu):
+    """Few rows over long sequences (the keys are split, a second kernel joins them), a padded batch: the launch is fixed when it is
+    captured, lengths and starts are read when it runs."""
+    w = World(gpu, 3, 2, 4, 128, torch.bfloat16, "int8", 64, seed=31)
+    k, v, _ = w.tokens(4000 + 1300)
+    w.append([4000, 1300, 0], k, v)
+    q = w.rand(40, w.Hq, w.D).to(w.dtype)
+    dq, out, scale = q.cuda(), torch.empty((40, w.Hq, 128), dtype=w.dtype, device="cuda:0"), 1 / math.sqrt(128)
+    lens, starts = _i32(w.lens), _starts([16, 16, 0])
+    side, ws, graph = torch.cuda.Stream(), w.cache.new_workspace(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        w.cache.attn_prefill(dq, scale, starts, lens, w.d_table, w.d_tails, max_new=16, out=out, workspace=ws)
+    for rows, back in (([16, 16, 0], (0, 0)), ([1, 0, 0], (0, 0)), ([3, 30, 0], (31, 9)), ([0, 40, 0], (5, 1)), ([16, 16, 0], (0, 0))):
+        now = [w.lens[0] - back[0], w.lens[1] - back[1], 0]
+        lens.copy_(_i32(now))
+        starts.copy_(_starts(rows))
+        out.fill_(7.)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graph.replay()
+        eager = torch.full_like(out, 7.)
+        w.cache.attn_prefill(dq, scale, starts, lens, w.d_table, w.d_tails, max_new=16, out=eager)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
+        was, w.lens = w.lens, now
+        want64 = _reference(w, rows, 0, scale, q)
+        w.lens = was
+        _close_chunks(out[:sum(rows)], *want64, w.dtype)
+        assert (out[sum(rows):] == 7).all()
+    w.check()
+
+
+def test_many_sequences_with_empty_places(gpu):
+    """More sequences than a wave has lanes, every third place empty, lengths around the ends of blocks."""
+    batch = 150
+    w = World(gpu, batch, 1, 2, 64, torch.float16, "int8", 3, seed=32)
+    counts = [0 if b % 3 == 2 else (1, 63, 64, 65, 127, 128, 129)[b % 7] for b in range(batch)]
+    k, v, q = w.tokens(sum(counts))
+    w.append(counts, k, v, q)
+    got = w.cache.attn_prefill(q.cuda(), 0.125, _starts(counts), _i32(w.lens), w.d_table, w.d_tails)
+    _close_chunks(got, *_reference(w, counts, 0, 0.125, q), w.dtype)
+    _decode(w, 1)
+    _decode(w, 3, window=70)
+    w.check()
+
+
+def test_the_binding_refuses(gpu):
+    cache = gpu.PagedCache(2, 4, 4, 2, head_dim=64)
+    seqs = (_i32([1]), _i32([[0, 1]]), _i32([0]))
+    k = torch.zeros((1, 2, 64), dtype=torch.float16, device="cuda:0")
+    q = torch.zeros((1, 4, 64), dtype=torch.float16, device="cuda:0")
+    for args, kw in (((k, k, *seqs), dict(q_out=q)), ((k, k, *seqs), dict(positions=_i32([[0]]))), ((k.float(), k, *seqs), {}), ((k.cpu(), k, *seqs), {}),
+                     ((k, q, *seqs), {}), ((k, k, seqs[0].long(), *seqs[1:]), {}), ((k, k, *seqs), dict(starts=_i32([0]))),
+                     ((k, k, seqs[0], seqs[1][0], seqs[2]), {}), ((k[:, :, ::2], k, *seqs), {})):
+        with pytest.raises(AssertionError):
+            cache.append(*args, **kw)
+    with pytest.raises(AssertionError):
+        cache.attn_decode(k, 0.1, *seqs)
+    with pytest.raises(AssertionError):
+        cache.attn_decode(q, 0.1, *seqs, workspace=torch.zeros(8, device="cuda:0"))
+    with pytest.raises(gpu.KvcompError):
+        cache.attn_decode(q, 0.1, *seqs, workspace=torch.zeros(8, dtype=torch.uint8, device="cuda:0"))
+    with pytest.raises(gpu.KvcompError):
+        cache.attn_decode(q, 0.1, *seqs, out=q)
+    with pytest.raises(gpu.KvcompError):
+        cache.attn_prefill(q, math.nan, _i32([0, 1]), *seqs)
+    cache.check()

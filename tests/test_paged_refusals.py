@@ -125,7 +125,7 @@ def test_null_structures(B):
 def _decode_args(B, **kw):
     lib = B.load()
     ws = lib.kvcomp_paged_workspace_bytes(_config(B))
-    d = dict(q=ALIGNED, q_stride=4096, q_len=1, scale=0.1, window=0, max_len=0, out=ALIGNED, out_stride=4096, ws=ALIGNED, ws_bytes=ws)
+    d = dict(q=ALIGNED, q_stride=4096, q_len=1, scale=0.1, window=0, max_len=0, out=2 * ALIGNED, out_stride=4096, ws=ALIGNED, ws_bytes=ws)
     d.update(kw)
     return [*d.values(), None]
 
@@ -133,7 +133,7 @@ def _decode_args(B, **kw):
 def _prefill_args(B, **kw):
     lib = B.load()
     ws = lib.kvcomp_paged_workspace_bytes(_config(B))
-    d = dict(q=ALIGNED, q_stride=4096, starts=ALIGNED, n_tokens=50, scale=0.1, window=0, max_new=0, max_len=0, out=ALIGNED,
+    d = dict(q=ALIGNED, q_stride=4096, starts=ALIGNED, n_tokens=50, scale=0.1, window=0, max_new=0, max_len=0, out=2 * ALIGNED,
              out_stride=4096, ws=ALIGNED, ws_bytes=ws)
     d.update(kw)
     return [*d.values(), None]
@@ -160,7 +160,7 @@ def test_attention_refuses_bad_caches(B, i):
 
 
 COMMON = [dict(q=0), dict(q=ALIGNED + 8), dict(q_stride=4088), dict(q_stride=4100), dict(out=0), dict(out=ALIGNED + 2), dict(out_stride=4000),
-          dict(scale=float("inf")), dict(scale=float("nan")), dict(window=-1), dict(max_len=-1), dict(ws=0), dict(ws=ALIGNED + 8)]
+          dict(scale=float("inf")), dict(scale=float("nan")), dict(scale=3e38), dict(window=-1), dict(max_len=-1), dict(ws=0), dict(ws=ALIGNED + 8)]
 
 
 @pytest.mark.parametrize("bad", COMMON + [dict(q_len=0), dict(q_len=-1), dict(q_len=9), dict(q_len=1 << 30)])
@@ -171,6 +171,32 @@ def test_decode_refuses_bad_arguments(B, bad):
 @pytest.mark.parametrize("bad", COMMON + [dict(starts=0), dict(starts=ALIGNED + 2), dict(n_tokens=-1), dict(n_tokens=1 << 26), dict(max_new=-1)])
 def test_prefill_refuses_bad_arguments(B, bad):
     _refused(B, B.load().kvcomp_paged_attn_prefill(_config(B), _memory(B), _batch(B), *_prefill_args(B, **bad)))
+
+
+@pytest.mark.parametrize("q,q_stride,out,out_stride,rows", [
+    (0, 4096, 0, 4096, 3), (0, 4096, 4080, 4096, 3), (0, 4096, 2 * 4096 + 4088, 4096, 3), (4088, 4096, 0, 4096, 1), (0, 8192, 4088, 8192, 3),
+    (0, 12288, 8200, 12288, 3), (12288 + 4088, 12288, 0, 12288, 3), (0, 4096, 4096, 8192, 3), (8, 12288, 0, 4096, 3)])
+def test_attention_refuses_outputs_over_queries(B, q, q_stride, out, out_stride, rows):
+    kw = dict(q=ALIGNED + 2 * q, out=ALIGNED + 2 * out, q_stride=q_stride, out_stride=out_stride)
+    seqs = _batch(B, batch=rows)
+    _refused(B, B.load().kvcomp_paged_attn_decode(_config(B), _memory(B), seqs, *_decode_args(B, **kw)))
+    _refused(B, B.load().kvcomp_paged_attn_prefill(_config(B), _memory(B), seqs, *_prefill_args(B, n_tokens=rows, **kw)))
+
+
+@pytest.mark.parametrize("q,q_stride,out,out_stride", [(0, 4096, 3 * 4096, 4096), (0, 12288, 4096, 12288), (8192, 12288, 0, 12288),
+                                                       (0, 12288, 2 * 12288 + 4096, 4096), (3 * 12288 + 4096, 12288, 0, 12288)])
+def test_attention_takes_slices_of_one_buffer(B, q, q_stride, out, out_stride):
+    """Up to the check behind it."""
+    kw = dict(q=ALIGNED + 2 * q, out=ALIGNED + 2 * out, q_stride=q_stride, out_stride=out_stride, ws_bytes=0)
+    assert B.load().kvcomp_paged_attn_decode(_config(B), _memory(B), _batch(B), *_decode_args(B, **kw)) == B.ERR_CAPACITY
+    assert B.load().kvcomp_paged_attn_prefill(_config(B), _memory(B), _batch(B), *_prefill_args(B, n_tokens=3, **kw)) == B.ERR_CAPACITY
+
+
+@pytest.mark.parametrize("bad", [dict(d_q_out=ALIGNED + 16), dict(d_q_out=5 * ALIGNED), dict(d_q_out=6 * ALIGNED - 16),
+                                 dict(q_stride=4096, q_out_stride=8192)])
+def test_append_refuses_rotated_queries_over_its_inputs(B, bad):
+    kw = dict(dict(Q, d_k=5 * ALIGNED, d_v=6 * ALIGNED), **bad)
+    _refused(B, B.load().kvcomp_paged_append(_config(B), _memory(B), _batch(B), _new(B, **kw), None))
 
 
 def test_attention_refuses_small_workspaces_and_large_batches(B):
