@@ -260,16 +260,22 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         if (masked) {
             const int low = p.a.window > 0 ? pos - p.a.window : -1;
 #pragma unroll
-            for (int j = 0; j < 2; j++)
+            for (int j = 0; j < 2; j++) {
+                seen[j] = 0;
+#pragma unroll
+                for (int x = 0; x < 2; x++) {  // eight keys in a row
+                    const int key = t * kPBT + 32 * j + 16 * x + 8 * half;
+                    const uint32_t upto = 1u << min(max(pos + 1 - key, 0), 8), below = 1u << min(max(low + 1 - key, 0), 8);
+                    seen[j] |= (upto - below) << (8 * x);
+                }
 #pragma unroll
                 for (int i = 0; i < 16; i++) {
-                    const int key = t * kPBT + 32 * j + 16 * (i >> 3) + 8 * half + (i & 7);
-                    if (key > pos || key <= low) {
-                        seen[j] &= ~(1u << i);
-                        s[j][i] = -INFINITY;
-                    }
+                    const uint32_t m = (uint32_t)((int32_t)(seen[j] << (31 - i)) >> 31);
+                    s[j][i] = __uint_as_float((m & __float_as_uint(s[j][i])) | (~m & 0xff800000u));
                 }
+            }
         }
+        const bool sees = (seen[0] | seen[1]) != 0, times_zero = !(f > 0.f);
         float mx = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 2; j++)
@@ -287,12 +293,13 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
             st.sum *= alpha;
             rescale(alpha * by_e);
         }
-        float off = mant - st.ref;
-        if (__builtin_amdgcn_ballot_w64(fabsf(mx) > kFarScore) != 0) {  // see above
+        const float ref = sees ? st.ref : 0.f;  // anything finite: all scores are -Inf
+        float off = mant - ref;
+        if (__builtin_amdgcn_ballot_w64(sees && fabsf(mx) > kFarScore) != 0) {  // see above
 #pragma unroll
             for (int j = 0; j < 2; j++)
 #pragma unroll
-                for (int i = 0; i < 16; i++) s[j][i] = s[j][i] * f - st.ref;
+                for (int i = 0; i < 16; i++) s[j][i] = s[j][i] * f - ref;
             f = 1.f;
             off = mant;
         }
@@ -305,7 +312,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
                 const float a = __builtin_amdgcn_exp2f(fmaf(s[j][i], f, off)), b = __builtin_amdgcn_exp2f(fmaf(s[j][i + 1], f, off));
                 pw[j][i >> 1] = narrow2<kF16>(a, b);
             }
-        if (masked) {  // whatever the powers of hidden scores came to (a scale of zero, a reference that nothing has set)
+        if (masked && __builtin_amdgcn_ballot_w64(times_zero) != 0) {  // -Inf times a scale of zero
 #pragma unroll
             for (int j = 0; j < 2; j++)
 #pragma unroll
