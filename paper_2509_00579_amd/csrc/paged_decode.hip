@@ -25,7 +25,9 @@ struct DecodeArgs {
     PagedGeo g;
     PagedAttn a;
     int q_len, rows;
+    uint32_t inv_g;  // 2^16 / G, rounded up: row * inv_g / 2^16 is row / G for the 32 rows that there are at most
 };
+__device__ __forceinline__ int place_of(const DecodeArgs &p, int row) { return (int)(((uint32_t)row * p.inv_g) >> 16); }
 
 __device__ __forceinline__ float4v mfma16(half8v a, half8v b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ half8v as_half8(uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
@@ -61,6 +63,10 @@ constexpr float kRefBelow = 15.f;
 // What an unfinished block costs, in pages: twice the bytes, and its loads start behind the pages'.  us with 3, 5, 8 pages: 8 x 8
 // heads of up to 16422 tokens 44.4 43.5 44.0, 64 x 8 of up to 1102 18.0 17.8 18.5, one head of 1000 11.2 11.5 11.8.
 constexpr int kTailUnits = 4;
+// Units that a workgroup has at least, while there are others without any: a wave alone on its SIMD is through with a page in less
+// than half the time of two.  us with 1, 2, 3, 4, 8 units: one head of 1000 9.7 9.2 9.4 9.7 10.9, 8 heads of 2000 in groups of 4 10.2
+// 9.8 10.1 10.5 12.6, one head in a group of 8 of 4000 14.6 11.8 11.4 11.1 12.7, 8 heads of 300 8.8 9.1 9.6 9.7 8.4.
+constexpr uint32_t kLeastUnits = 2;
 // bf16: the accumulators hold 2^-40 of the sums, so that neither the largest values overflow them (2^15 of a weight, 2^26 keys)
 // nor the largest weight's of anything that a page holds (2^-100 and more) drops below binary32's normal range; the factor
 // is a multiplication of its own, since with it the smallest scales would.
@@ -85,7 +91,7 @@ struct Wave {
 
     __device__ __forceinline__ Wave(const DecodeArgs &p_, int lane_) : p(p_), lane(lane_), n(lane_ & 15), g4(lane_ >> 4) {
 #pragma unroll
-        for (int r = 0; r < R; r++) q_place[r] = (16 * r + n) / p.g.G;
+        for (int r = 0; r < R; r++) q_place[r] = place_of(p, 16 * r + n);
     }
 
     // A head's queries are asked for, and made ready once something else is on its way too.
@@ -409,7 +415,7 @@ constexpr size_t kDecodeLdsBytes = 159 * 1024;  // what the kernels may have apa
 template <int T, int D>
 __device__ __forceinline__ void store_row4(const DecodeArgs &p, int b, int h, int row, int c, const float (&o)[4], float sum) {
     const float f = sum == 0.f ? 0.f : (1.f / kVUnit<T>) / sum;
-    const int place = row / p.g.G;
+    const int place = place_of(p, row);
     uint16_t *out = p.a.out + ((size_t)b * p.q_len + place) * p.a.out_stride + (size_t)(h * p.g.G + row - place * p.g.G) * D + c;
     *reinterpret_cast<uint2 *>(out) = make_uint2(narrow2<T>(o[0] * f, o[1] * f), narrow2<T>(o[2] * f, o[3] * f));
 }
@@ -465,8 +471,7 @@ __global__ __launch_bounds__(64 * W) void paged_decode_kernel(DecodeArgs p) {
         }
     };
     const uint32_t H = p.g.H, total = sum * H;
-    // no more workgroups than there is work for their waves
-    const uint32_t active = min((uint32_t)gridDim.x, (total + kWaves - 1) / kWaves), wg = blockIdx.x;
+    const uint32_t active = min((uint32_t)gridDim.x, (total + kLeastUnits - 1) / kLeastUnits), wg = blockIdx.x;
     if (wg >= active) {
         fill_empty();
         return;
@@ -651,7 +656,7 @@ hipError_t launch_waves(const DecodeArgs &p, int max_len, hipStream_t s) {
     if (lds > kDecodeLdsBytes) return hipErrorInvalidValue;
     // units of work that there could be: no more workgroups than they can busy
     const int pages = max_len > 0 && max_len < p.g.max_pages * kPBT ? (max_len + kPBT - 1) / kPBT : p.g.max_pages;
-    const size_t most = (size_t)p.g.batch * p.g.H * (pages + kTailUnits), wgs = (most + W - 1) / W;
+    const size_t most = (size_t)p.g.batch * p.g.H * (pages + kTailUnits), wgs = (most + kLeastUnits - 1) / kLeastUnits;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(wgs < (size_t)kDecodeWGs ? wgs : (size_t)kDecodeWGs)), dim3(kThreads), lds, s, p);
     return hipGetLastError();
 }
@@ -668,7 +673,7 @@ hipError_t launch(const DecodeArgs &p, int max_len, hipStream_t s) {
 
 hipError_t launch_paged_decode(const PagedGeo &g, const PagedAttn &a, int q_len, int max_len, int head_dim, int data_type, int code_type,
                                hipStream_t s) {
-    DecodeArgs p = {g, a, q_len, q_len * g.G};
+    DecodeArgs p = {g, a, q_len, q_len * g.G, (65536u + g.G - 1) / g.G};
     auto by_rows = [&](auto t, auto c, auto d) {
         if (p.rows <= 16) return launch<decltype(t)::value, decltype(c)::value, decltype(d)::value, 1>(p, max_len, s);
         return launch<decltype(t)::value, decltype(c)::value, decltype(d)::value, 2>(p, max_len, s);
