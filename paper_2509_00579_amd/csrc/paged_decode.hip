@@ -538,27 +538,28 @@ __global__ __launch_bounds__(64 * W) void paged_decode_kernel(DecodeArgs p) {
         for (int item = tid; item < p.rows * kQuads; item += kThreads) {
             const int row = item / kQuads, c = (item - row * kQuads) * 4;
             const float *at = s_dyn + row * kPitch;
+            // everything on its way at once; what other heads' slots and empty ones hold is left out behind
             float m[kSlots], l[kSlots];
+            float4 v[kSlots];
 #pragma unroll
             for (int s = 0; s < kSlots; s++) {
-                const bool have = (mine >> s) & 1;
-                m[s] = have ? at[s * slot_floats + D] : -INFINITY;
-                l[s] = have ? at[s * slot_floats + D + 1] : 0.f;
+                m[s] = at[s * slot_floats + D];
+                l[s] = at[s * slot_floats + D + 1];
+                v[s] = *reinterpret_cast<const float4 *>(at + s * slot_floats + c);
             }
             float top = kLowestRef;
 #pragma unroll
-            for (int s = 0; s < kSlots; s++) top = fmaxf(top, m[s]);
+            for (int s = 0; s < kSlots; s++) top = fmaxf(top, (mine >> s) & 1 ? m[s] : -INFINITY);
             float sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int s = 0; s < kSlots; s++) {
-                if (!((mine >> s) & 1)) continue;
-                const float f = __builtin_amdgcn_exp2f(m[s] - top);
-                const float4 v = *reinterpret_cast<const float4 *>(at + s * slot_floats + c);
-                sum = fmaf(l[s], f, sum);
-                acc[0] = fmaf(v.x, f, acc[0]);
-                acc[1] = fmaf(v.y, f, acc[1]);
-                acc[2] = fmaf(v.z, f, acc[2]);
-                acc[3] = fmaf(v.w, f, acc[3]);
+                const bool have = (mine >> s) & 1;
+                const float f = have ? __builtin_amdgcn_exp2f(m[s] - top) : 0.f;
+                sum = fmaf(have ? l[s] : 0.f, f, sum);
+                acc[0] = fmaf(have ? v[s].x : 0.f, f, acc[0]);
+                acc[1] = fmaf(have ? v[s].y : 0.f, f, acc[1]);
+                acc[2] = fmaf(have ? v[s].z : 0.f, f, acc[2]);
+                acc[3] = fmaf(have ? v[s].w : 0.f, f, acc[3]);
             }
             if (complete) {
                 store_row4<T, D>(p, sb, sh, row, c, acc, sum);
@@ -592,7 +593,7 @@ __global__ __launch_bounds__(64 * W) void paged_decode_kernel(DecodeArgs p) {
         if (!s_last[k]) continue;
         // The last to arrive: groups of threads take the parts in turn, everything that a thread needs of four parts on its way at
         // once; the groups meet in LDS.
-        const int items = p.rows * kQuads, groups = max(1, min(kThreads / items, (int)parts));
+        const int items = p.rows * kQuads, groups = max(1, min(kThreads / items, (int)(parts + 3) / 4));
         for (int at = 0; at < items; at += kThreads) {  // one round, unless there are more items than threads
             const int local = groups > 1 ? tid % items : tid, group = groups > 1 ? tid / items : 0, item = at + local;
             const bool live = item < items && group < groups;
@@ -609,16 +610,25 @@ __global__ __launch_bounds__(64 * W) void paged_decode_kernel(DecodeArgs p) {
                         lo[x] = load_agent2(v + c);
                         hi[x] = load_agent2(v + c + 2);
                     }
+                    float now = top;
 #pragma unroll
                     for (int x = 0; x < 4; x++) {
-                        if (i + x * groups >= parts) continue;
-                        const float now = fmaxf(top, ml[x].x), old = __builtin_amdgcn_exp2f(top - now), f = __builtin_amdgcn_exp2f(ml[x].x - now);
-                        top = now;
-                        total_l = fmaf(ml[x].y, f, total_l * old);
-                        acc[0] = fmaf(lo[x].x, f, acc[0] * old);
-                        acc[1] = fmaf(lo[x].y, f, acc[1] * old);
-                        acc[2] = fmaf(hi[x].x, f, acc[2] * old);
-                        acc[3] = fmaf(hi[x].y, f, acc[3] * old);
+                        if (i + x * groups >= parts) ml[x] = make_float2(-INFINITY, 0.f);
+                        now = fmaxf(now, ml[x].x);
+                    }
+                    const float old = __builtin_amdgcn_exp2f(top - now);
+                    top = now;
+                    total_l *= old;
+#pragma unroll
+                    for (int y = 0; y < 4; y++) acc[y] *= old;
+#pragma unroll
+                    for (int x = 0; x < 4; x++) {
+                        const float f = __builtin_amdgcn_exp2f(ml[x].x - now);
+                        total_l = fmaf(ml[x].y, f, total_l);
+                        acc[0] = fmaf(lo[x].x, f, acc[0]);
+                        acc[1] = fmaf(lo[x].y, f, acc[1]);
+                        acc[2] = fmaf(hi[x].x, f, acc[2]);
+                        acc[3] = fmaf(hi[x].y, f, acc[3]);
                     }
                 }
             }
