@@ -538,28 +538,36 @@ __global__ __launch_bounds__(64 * W) void paged_decode_kernel(DecodeArgs p) {
         for (int item = tid; item < p.rows * kQuads; item += kThreads) {
             const int row = item / kQuads, c = (item - row * kQuads) * 4;
             const float *at = s_dyn + row * kPitch;
-            // everything on its way at once; what other heads' slots and empty ones hold is left out behind
-            float m[kSlots], l[kSlots];
-            float4 v[kSlots];
+            float top = kLowestRef, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+            for (uint32_t rest = mine; rest;) {  // four states on their way at once
+                float m[4], l[4];
+                float4 v[4];
+                float now = top;
 #pragma unroll
-            for (int s = 0; s < kSlots; s++) {
-                m[s] = at[s * slot_floats + D];
-                l[s] = at[s * slot_floats + D + 1];
-                v[s] = *reinterpret_cast<const float4 *>(at + s * slot_floats + c);
-            }
-            float top = kLowestRef;
+                for (int x = 0; x < 4; x++) {
+                    const bool have = rest != 0;
+                    const float *from = at + (have ? __builtin_ctz(rest) : s0) * slot_floats;
+                    rest &= rest - 1;
+                    m[x] = have ? from[D] : -INFINITY;
+                    l[x] = from[D + 1];
+                    v[x] = *reinterpret_cast<const float4 *>(from + c);
+                }
 #pragma unroll
-            for (int s = 0; s < kSlots; s++) top = fmaxf(top, (mine >> s) & 1 ? m[s] : -INFINITY);
-            float sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+                for (int x = 0; x < 4; x++) now = fmaxf(now, m[x]);
+                float f = __builtin_amdgcn_exp2f(top - now);
+                top = now;
+                sum *= f;
 #pragma unroll
-            for (int s = 0; s < kSlots; s++) {
-                const bool have = (mine >> s) & 1;
-                const float f = have ? __builtin_amdgcn_exp2f(m[s] - top) : 0.f;
-                sum = fmaf(have ? l[s] : 0.f, f, sum);
-                acc[0] = fmaf(have ? v[s].x : 0.f, f, acc[0]);
-                acc[1] = fmaf(have ? v[s].y : 0.f, f, acc[1]);
-                acc[2] = fmaf(have ? v[s].z : 0.f, f, acc[2]);
-                acc[3] = fmaf(have ? v[s].w : 0.f, f, acc[3]);
+                for (int k = 0; k < 4; k++) acc[k] *= f;
+#pragma unroll
+                for (int x = 0; x < 4; x++) {
+                    f = __builtin_amdgcn_exp2f(m[x] - now);
+                    sum = fmaf(l[x], f, sum);
+                    acc[0] = fmaf(v[x].x, f, acc[0]);
+                    acc[1] = fmaf(v[x].y, f, acc[1]);
+                    acc[2] = fmaf(v[x].z, f, acc[2]);
+                    acc[3] = fmaf(v[x].w, f, acc[3]);
+                }
             }
             if (complete) {
                 store_row4<T, D>(p, sb, sh, row, c, acc, sum);
