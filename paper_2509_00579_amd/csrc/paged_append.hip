@@ -136,7 +136,7 @@ constexpr int kQRows = 2;
 constexpr int kVPitch = 17;      // words of a V channel in LDS: 16, and one so that the writers of eight channels hit eight banks
 
 template <int T, int C, int D>
-__global__ __launch_bounds__(kRowGroups * D / 16) void paged_append_kernel(PagedGeo g, PagedNew n, int block_units) {
+__global__ __launch_bounds__(kRowGroups * D / 16) void paged_append_kernel(PagedGeo g, PagedNew n, int block_units, Divide by_heads, Divide by_q_heads) {
     constexpr int kItems = D / 16, kThreads = kRowGroups * kItems;
     __shared__ uint32_t s_v[D * kVPitch];
     __shared__ uint32_t s_max[2][2];
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(kRowGroups * D / 16) void paged_append_kernel(Paged
 #pragma unroll
         for (int k = 0; k < kQRows; k++) {
             const uint32_t r = r0 + k;
-            tok[k] = (int)(r / (uint32_t)Hq);
+            tok[k] = (int)by_q_heads.of(r);
             head[k] = (int)(r - (uint32_t)tok[k] * (uint32_t)Hq);
             if (r >= rows || tok[k] >= n_used || tok[k] < n_first) tok[k] = -1;
             if (tok[k] < 0) continue;
@@ -212,7 +212,7 @@ __global__ __launch_bounds__(kRowGroups * D / 16) void paged_append_kernel(Paged
     }
 
     // which block of which sequence
-    int unit = blockIdx.x / g.H;
+    int unit = (int)by_heads.of(blockIdx.x);
     const int h = blockIdx.x - unit * g.H;
     int b, start, fresh, len;  // first new row, new tokens
     bool bad = false;
@@ -436,7 +436,7 @@ void launch(const PagedGeo &g, PagedNew n, hipStream_t s) {
     n.stream_q = q_rows * D * 2 > (size_t)32 << 20;
     const size_t q_units = (q_rows + kRowGroups * kQRows - 1) / (kRowGroups * kQRows);
     hipLaunchKernelGGL((paged_append_kernel<T, C, D>), dim3((unsigned)(most * g.H + q_units)), dim3(kRowGroups * D / 16), 0, s, g, n,
-                       (int)(most * g.H));
+                       (int)(most * g.H), Divide(g.H), Divide(g.H * g.G));
 }
 
 }  // namespace

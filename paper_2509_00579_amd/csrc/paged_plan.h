@@ -25,6 +25,18 @@ struct Deal {
     }
 };
 
+// Division of numbers below 2^31 by one that the host knows: m is 2^(31 + s) / d rounded up, s the bits of d - 1, so m has 32 bits and is
+// too large by less than 2^s / 2^(31 + s) of itself.  (A division by a number in a register is some twenty instructions one after the other.)
+struct Divide {
+    uint32_t m, shift;
+    Divide() = default;
+    KVC_BOTH explicit Divide(uint32_t d) : m(0), shift(31) {
+        while ((1ull << (shift - 31)) < d) shift++;
+        m = (uint32_t)(((1ull << shift) + d - 1) / d);
+    }
+    KVC_BOTH uint32_t of(uint32_t n) const { return (uint32_t)(((uint64_t)n * m) >> shift); }
+};
+
 // Tiles of 64 tokens that query rows at positions len - q_len .. len - 1 have to look at: from `first`, `count` of them.
 struct TileRange {
     int first, count;

@@ -39,6 +39,7 @@ struct PrefillArgs {
     int n_tokens, units, splits;
     int per_tile;  // tokens of a row tile
     const int32_t *__restrict__ starts;
+    Divide by_heads, by_splits, by_group, by_tile;
 };
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -64,7 +65,7 @@ __device__ __forceinline__ RowTile find_tile(const PrefillArgs &p, int unit, int
             len = p.g.lens[base + lane];
             tail = p.g.tails[base + lane];
             asm volatile("" ::"v"(len), "v"(tail));
-            if (s0 >= 0 && s1 > s0 && s1 <= p.n_tokens) tiles = (s1 - s0 + p.per_tile - 1) / p.per_tile;
+            if (s0 >= 0 && s1 > s0 && s1 <= p.n_tokens) tiles = (int)p.by_tile.of(s1 - s0 + p.per_tile - 1);
             else if (s1 != s0 || s0 < 0 || s1 > p.n_tokens) flag(p.g.fault, kFaultLength);
         }
         const int before = (int)wave_excl_scan((uint32_t)tiles, lane);
@@ -164,10 +165,11 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
     constexpr int kUnits = kPBT * D / 8, kPieces = (kPBT * D / 16 + kPreThreads - 1) / kPreThreads;  // 16-byte units of a tile; pieces of 16 codes per thread
     extern __shared__ __align__(16) uint4 s_tiles[];  // [2 buffers][K, V][kUnits]
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n = lane & 31, half = lane >> 5;
-    const int h = uniform(blockIdx.x % p.g.H), rest = uniform(blockIdx.x / p.g.H), split = uniform(rest % p.splits), unit = p.units - 1 - uniform(rest / p.splits);
+    const int rest = (int)p.by_heads.of(blockIdx.x), h = (int)blockIdx.x - rest * p.g.H, from_last = (int)p.by_splits.of(rest);
+    const int split = rest - from_last * p.splits, unit = p.units - 1 - from_last;
     const RowTile rt = find_tile(p, unit, lane);
     if (rt.b < 0) return;
-    const int G = p.g.G, r = 32 * wave + n, place = rt.place + r / G, head = h * G + r % G;
+    const int G = p.g.G, r = 32 * wave + n, in_tile = (int)p.by_group.of(r), place = rt.place + in_tile, head = h * G + r - in_tile * G;
     const bool live = r < p.per_tile * G && place < rt.fresh;
     const int past = rt.len - rt.fresh;
     const int pos = live ? past + place : -1;
@@ -178,7 +180,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
     const int blocks = rt.bad || last_pos < 0 ? 0 : last_pos / kPBT + 1 - from;
     const int unfinished = rt.len / kPBT;  // this block is in 16 bits
     const int shares = blocks + (from + blocks > unfinished ? kTailBlocks - 1 : 0);
-    auto share = [&](int k) { return uniform(from + min((int)((long long)shares * k / p.splits), blocks)); };
+    auto share = [&](int k) { return uniform(from + min((int)p.by_splits.of(shares * k), blocks)); };
     const int t0 = share(split), t1 = share(split + 1);
 
     constexpr int KS = D / 16;
@@ -224,8 +226,8 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
 
     const int token_row = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);  // of K's 32, see above
     // the last key that this wave's rows see, and the first row's
-    const int wave_last = uniform(past + min(rt.place + min(32 * wave + 31, p.per_tile * G - 1) / G, rt.fresh - 1));
-    const int wave_first = uniform(past + rt.place + 32 * wave / G);
+    const int wave_last = uniform(past + min(rt.place + (int)p.by_group.of(min(32 * wave + 31, p.per_tile * G - 1)), rt.fresh - 1));
+    const int wave_first = uniform(past + rt.place + (int)p.by_group.of(32 * wave));
     auto some_hidden = [&](int t) { return t * kPBT + kPBT - 1 > wave_first || (p.a.window > 0 && t * kPBT <= wave_last - p.a.window); };
 
     float16v s[2];       // scores
@@ -570,11 +572,12 @@ template <int T, int D>
 __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PrefillArgs p, int tile_rows) {
     constexpr int kMine = D / 64, kBatch = 8;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-    const int groups = tile_rows / kJoinWaves, group = uniform(blockIdx.x % groups), rest = uniform(blockIdx.x / groups);
-    const int h = uniform(rest % p.g.H), unit = uniform(rest / p.g.H), r = group * kJoinWaves + wave;
+    const uint32_t groups = tile_rows / kJoinWaves;  // a power of two
+    const int group = blockIdx.x & (groups - 1), rest = blockIdx.x >> __builtin_ctz(groups);
+    const int unit = (int)p.by_heads.of(rest), h = rest - unit * p.g.H, r = group * kJoinWaves + wave, in_tile = (int)p.by_group.of(r);
     const RowTile rt = find_tile(p, unit, lane);
     if (rt.b < 0) return;
-    const int place = uniform(rt.place + r / p.g.G);
+    const int place = rt.place + in_tile;
     if (r >= p.per_tile * p.g.G || place >= rt.fresh) return;
     const float *part = p.a.partials + ((size_t)(unit * p.g.H + h) * p.splits * tile_rows + r) * partial_pitch(D);
     const size_t step = (size_t)tile_rows * partial_pitch(D);
@@ -602,7 +605,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PrefillArgs
             for (int c = 0; c < kMine; c++) o[c] = fmaf(v[k][c], bcast(w, (s + k) & 63), o[c]);
     }
     const float by = sum == 0.f ? 0.f : 1.f / sum, unit_v = ldexpf(1.f, (int)e_top);
-    uint16_t *out = p.a.out + (size_t)(rt.start + place) * p.a.out_stride + (size_t)(h * p.g.G + r % p.g.G) * D + lane * kMine;
+    uint16_t *out = p.a.out + (size_t)(rt.start + place) * p.a.out_stride + (size_t)(h * p.g.G + r - in_tile * p.g.G) * D + lane * kMine;
     if constexpr (D == 128) *reinterpret_cast<uint32_t *>(out) = narrow2<T>(o[0] * by * unit_v, o[1] * by * unit_v);
     else *out = (uint16_t)narrow2<T>(o[0] * by * unit_v, 0.f);
 }
@@ -637,6 +640,10 @@ hipError_t launch_tiles(PrefillArgs p, int max_len, hipStream_t s) {
             p.splits = k;
         }
     }
+    p.by_heads = Divide(p.g.H);
+    p.by_splits = Divide(p.splits);
+    p.by_group = Divide(p.g.G);
+    p.by_tile = Divide(p.per_tile);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(base * p.splits)), dim3(64 * W), kLds, s, p);
     if (p.splits > 1)
         hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3((unsigned)(base * (32 * W / kJoinWaves))), dim3(64 * kJoinWaves), 0, s, p, 32 * W);

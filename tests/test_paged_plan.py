@@ -60,3 +60,35 @@ def test_every_tile_has_one_owner(tmp_path):
                     "-fno-sanitize-recover=all", str(src), "-o", str(exe)], check=True)
     r = subprocess.run([str(exe)], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
     assert r.returncode == 0 and "ok" in r.stdout, r.stdout[-2000:]
+
+
+DIVIDE = r"""
+#include <cstdio>
+#include <cstdlib>
+#include "../paper_2509_00579_amd/csrc/paged_plan.h"
+using namespace kvc;
+static void check(unsigned d, unsigned n) {
+    if (Divide(d).of(n) != n / d) { printf("%u / %u\n", n, d); exit(1); }
+}
+int main() {
+    for (unsigned d = 1; d < (1u << 30); d += d < 5000 ? 1 : d / 97) {
+        for (unsigned n = 0; n < 300; n++) check(d, n);
+        for (unsigned k = 1; k && k <= 0x7fffffffu / d; k += 1 + k / 3)
+            for (int off = -1; off <= 1; off++) check(d, k * d + off > 0x7fffffffu ? 0x7fffffffu : k * d + off);
+        const unsigned last = 0x7fffffffu / d * d;
+        check(d, last); check(d, last - 1); check(d, 0x7fffffffu); check(d, 0x7ffffffeu);
+    }
+    puts("ok");
+}
+"""
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+def test_division_by_multiplication(tmp_path):
+    src = tmp_path / "divide.cc"
+    src.write_text(DIVIDE.replace("../paper_2509_00579_amd", str(ROOT / "paper_2509_00579_amd")))
+    exe = tmp_path / "divide"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Wextra", "-Werror", "-fsanitize=address,undefined",
+                    "-fno-sanitize-recover=all", str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], stdout=subprocess.PIPE, text=True, timeout=60)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout
