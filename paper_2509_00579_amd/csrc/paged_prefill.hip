@@ -623,19 +623,23 @@ hipError_t launch_tiles(PrefillArgs p, int max_len, hipStream_t s) {
     p.units = p.n_tokens / p.per_tile + some;
     const long long base = (long long)p.units * p.g.H;
     const int pages = max_len > 0 && max_len < p.g.max_pages * kPBT ? (max_len + kPBT - 1) / kPBT : p.g.max_pages;
-    // Splits of the keys, by what they would take in blocks per CU: the row tiles that there are likely to be, in rounds where one
-    // workgroup fills a CU (several share its time evenly), at least the longest one, and what a split costs by itself (its
-    // state's way to memory and back).  4 chunks of 16 tokens on 4001, 8 KV heads, groups of 4, with 4, 6, 8, 12, 15, 20 splits:
-    // 39.7 33.0 29.3 32.4 30.7 38.3 us.
+    // Splits of the keys, by what they would take, in blocks on a CU: a workgroup has its share of the longest range (an unfinished
+    // block counts for more, see above) and what it does before the first and behind the last block; workgroups that have to wait
+    // for others are rounds, those that run beside others on a CU slow them down; the join reads every state.  A split more has to
+    // be worth it.  us with 1, 2, 4, 6, 8, 11, 16 splits: a chunk of 16 tokens on 484 (8 KV heads, groups of 4) 19.2 15.8 13.3 13.7
+    // 12.5, 4 of 16 on 984 31.1 23.3 18.7 17.7 18.9 22.4 23.9, 4 of 16 on 4001 102 58.3 35.3 29.1 26.2 28.0 26.9.
     const double tiles = std::max<double>(some, (p.n_tokens + p.per_tile - 1) / p.per_tile + 0.5 * (some - 1)) * p.g.H;
     const double longest = p.a.window > 0 ? std::min<double>(pages, (p.a.window + p.per_tile) / kPBT + 2) : pages;
     const double mean = std::max(longest / 2, longest - (double)p.n_tokens / some / kPBT / 2);
+    constexpr double kAround = 3, kBeside = D == 128 ? 0.75 : 0.6;
     double best = 0;
     p.splits = 1;
-    for (int k = 1; k <= kMaxKeySplits && (k == 1 || (k * 4 <= longest && base * k * 32 * W <= kPrefillStateRows)); k++) {
-        const double share = tiles * k / 256, rounds = std::max(1.0, workgroups_per_cu(D, W) == 1 ? std::ceil(share) : share), extra = k == 1 ? 0 : 3 * rounds + 6 + 0.1 * k;
-        const double cost = std::max(rounds * mean / k, longest / k) + extra;
-        if (k == 1 || cost < best) {
+    for (int k = 1; k <= kMaxKeySplits && k <= longest && (k == 1 || base * k * 32 * W <= kPrefillStateRows); k++) {
+        const double share = tiles * k / 256;
+        const double rounds = share <= 1 ? 1 : workgroups_per_cu(D, W) == 1 ? std::ceil(share) : std::max(1.5, kBeside * share);
+        auto work = [&](double blocks) { return kAround + std::ceil((blocks + kTailBlocks - 1) / k); };
+        const double cost = std::max(rounds * work(mean), work(longest)) + (k == 1 ? 0 : 3 + 0.1 * k + 0.005 * k * tiles);
+        if (k == 1 || cost < 0.95 * best) {
             best = cost;
             p.splits = k;
         }
