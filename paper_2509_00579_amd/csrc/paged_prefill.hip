@@ -565,49 +565,68 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
     }
 }
 
-// Joins the splits of a row tile: one wave per row, D / 64 channels a lane.  Lane s has the state of split s, so all weights are
-// known after one load; the accumulators of eight splits are on their way together.
+// Joins the splits of a row tile: R rows per wave, their loads on the way together, D / 64 channels a lane.  Lane s has the states of
+// split s, so all weights of a row are known after one load.
 constexpr int kJoinWaves = 4, kMaxKeySplits = 64;
-template <int T, int D>
+template <int T, int D, int R>
 __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PrefillArgs p, int tile_rows) {
-    constexpr int kMine = D / 64, kBatch = 8;
+    constexpr int kMine = D / 64, kJoinRows = R, kBatch = R == 1 ? 8 : 4;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-    const uint32_t groups = tile_rows / kJoinWaves;  // a power of two
+    const uint32_t groups = tile_rows / (kJoinWaves * kJoinRows);  // a power of two
     const int group = blockIdx.x & (groups - 1), rest = blockIdx.x >> __builtin_ctz(groups);
-    const int unit = (int)p.by_heads.of(rest), h = rest - unit * p.g.H, r = group * kJoinWaves + wave, in_tile = (int)p.by_group.of(r);
+    const int unit = (int)p.by_heads.of(rest), h = rest - unit * p.g.H, r0 = (group * kJoinWaves + wave) * kJoinRows;
     const RowTile rt = find_tile(p, unit, lane);
     if (rt.b < 0) return;
-    const int place = rt.place + in_tile;
-    if (r >= p.per_tile * p.g.G || place >= rt.fresh) return;
-    const float *part = p.a.partials + ((size_t)(unit * p.g.H + h) * p.splits * tile_rows + r) * partial_pitch(D);
+    const int rows = min(p.per_tile, rt.fresh - rt.place) * p.g.G - r0;  // that there are from here on
+    if (rows <= 0) return;
+    const float *part = p.a.partials + ((size_t)(unit * p.g.H + h) * p.splits * tile_rows + r0) * partial_pitch(D);
     const size_t step = (size_t)tile_rows * partial_pitch(D);
-    float m = -INFINITY, l = 0.f, e = -140.f;
-    if (lane < p.splits) {
-        const float4 s = *reinterpret_cast<const float4 *>(part + lane * step + D);
-        m = s.x;
-        l = s.y;
-        e = s.z;
-    }
-    const float top = wave_max(m), e_top = wave_max(e);
-    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-    const float sum = wave_sum(m == -INFINITY ? (l != l ? l : 0.f) : l * f);  // a split that met nothing takes no part
-    const float w = f * __builtin_amdgcn_exp2f(e - e_top);
-    float o[kMine] = {};
-    for (int s = 0; s < p.splits; s += kBatch) {
-        float v[kBatch][kMine];
+    float4 state[kJoinRows];
+#pragma unroll
+    for (int i = 0; i < kJoinRows; i++)
+        state[i] = lane < p.splits && i < rows ? *reinterpret_cast<const float4 *>(part + lane * step + i * partial_pitch(D) + D)
+                                               : make_float4(-INFINITY, 0.f, -140.f, 0.f);
+    float w[kJoinRows], by[kJoinRows], unit_v[kJoinRows], o[kJoinRows][kMine] = {};
+    auto fetch = [&](int s, float (&v)[kBatch][kJoinRows][kMine]) __attribute__((always_inline)) {
 #pragma unroll
         for (int k = 0; k < kBatch; k++)
 #pragma unroll
-            for (int c = 0; c < kMine; c++) v[k][c] = s + k < p.splits ? part[(s + k) * step + lane * kMine + c] : 0.f;
+            for (int i = 0; i < kJoinRows; i++)
+#pragma unroll
+                for (int c = 0; c < kMine; c++)
+                    v[k][i][c] = s + k < p.splits && i < rows ? part[(s + k) * step + i * partial_pitch(D) + lane * kMine + c] : 0.f;
+    };
+    float v[kBatch][kJoinRows][kMine];
+    fetch(0, v);
+#pragma unroll
+    for (int i = 0; i < kJoinRows; i++) {
+        const float m = state[i].x, l = state[i].y, e = state[i].z;
+        const float top = wave_max(m), e_top = wave_max(e);
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        const float sum = wave_sum(m == -INFINITY ? (l != l ? l : 0.f) : l * f);  // a split that met nothing takes no part
+        w[i] = f * __builtin_amdgcn_exp2f(e - e_top);
+        by[i] = sum == 0.f ? 0.f : 1.f / sum;
+        unit_v[i] = ldexpf(1.f, (int)e_top);
+    }
+    for (int s = 0;;) {
 #pragma unroll
         for (int k = 0; k < kBatch; k++)
 #pragma unroll
-            for (int c = 0; c < kMine; c++) o[c] = fmaf(v[k][c], bcast(w, (s + k) & 63), o[c]);
+            for (int i = 0; i < kJoinRows; i++)
+#pragma unroll
+                for (int c = 0; c < kMine; c++) o[i][c] = fmaf(v[k][i][c], bcast(w[i], (s + k) & 63), o[i][c]);
+        s += kBatch;
+        if (s >= p.splits) break;
+        fetch(s, v);
     }
-    const float by = sum == 0.f ? 0.f : 1.f / sum, unit_v = ldexpf(1.f, (int)e_top);
-    uint16_t *out = p.a.out + (size_t)(rt.start + place) * p.a.out_stride + (size_t)(h * p.g.G + r - in_tile * p.g.G) * D + lane * kMine;
-    if constexpr (D == 128) *reinterpret_cast<uint32_t *>(out) = narrow2<T>(o[0] * by * unit_v, o[1] * by * unit_v);
-    else *out = (uint16_t)narrow2<T>(o[0] * by * unit_v, 0.f);
+#pragma unroll
+    for (int i = 0; i < kJoinRows; i++) {
+        if (i >= rows) break;
+        const int r = r0 + i, in_tile = (int)p.by_group.of(r);
+        uint16_t *out = p.a.out + (size_t)(rt.start + rt.place + in_tile) * p.a.out_stride + (size_t)(h * p.g.G + r - in_tile * p.g.G) * D + lane * kMine;
+        if constexpr (D == 128) *reinterpret_cast<uint32_t *>(out) = narrow2<T>(o[i][0] * by[i] * unit_v[i], o[i][1] * by[i] * unit_v[i]);
+        else *out = (uint16_t)narrow2<T>(o[i][0] * by[i] * unit_v[i], 0.f);
+    }
 }
 
 template <int T, int C, int D, int W>
@@ -649,8 +668,14 @@ hipError_t launch_tiles(PrefillArgs p, int max_len, hipStream_t s) {
     p.by_group = Divide(p.g.G);
     p.by_tile = Divide(p.per_tile);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(base * p.splits)), dim3(64 * W), kLds, s, p);
-    if (p.splits > 1)
-        hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3((unsigned)(base * (32 * W / kJoinWaves))), dim3(64 * kJoinWaves), 0, s, p, 32 * W);
+    if (p.splits > 1) {
+        // One row per wave while all waves are on the chip at once, or twice; four share the work around them.  us of the whole
+        // call with one, four: 4 chunks of 16 tokens on 4001 (6144 rows) 25.6 26.7, one of 8 on 30 k 26.1 35.0; 16 of 16 on 1984
+        // (24576 rows) 42.8 40.4, 512 tokens on 32 k (34816) 532 527, 32 of 16 on 3984, heads of 64 (49152) 71.4 65.0.
+        const long long rows = base * 32 * W;
+        if (rows > 16384) hipLaunchKernelGGL((paged_join_kernel<T, D, 4>), dim3((unsigned)(rows / (kJoinWaves * 4))), dim3(64 * kJoinWaves), 0, s, p, 32 * W);
+        else hipLaunchKernelGGL((paged_join_kernel<T, D, 1>), dim3((unsigned)(rows / kJoinWaves)), dim3(64 * kJoinWaves), 0, s, p, 32 * W);
+    }
     return hipGetLastError();
 }
 

@@ -803,6 +803,21 @@ def test_prefill_captured_on_another_stream_and_replayed_with_other_lengths(gpu)
     w.check()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_prefill_many_rows_of_split_keys(gpu, D):
+    """Chunks of 16 sequences whose keys are still worth splitting: the join takes four rows a wave, ragged ends among them."""
+    w = World(gpu, 16, 8, 4, D, torch.float16 if D == 64 else torch.bfloat16, "int8", 14, seed=33)
+    counts = [(400 + 37 * b) % 830 for b in range(16)]
+    k, v, _ = w.tokens(sum(counts))
+    w.append(counts, k, v)
+    rows = [(10, 16, 0, 1, 3, 33, 9, 15)[b % 8] for b in range(16)]
+    k, v, _ = w.tokens(sum(rows))
+    w.append(rows, k, v)
+    _prefill(w, rows)
+    _prefill(w, rows, window=200)
+    w.check()
+
+
 def test_many_sequences_with_empty_places(gpu):
     """More sequences than a wave has lanes, every third place empty, lengths around the ends of blocks."""
     batch = 150
