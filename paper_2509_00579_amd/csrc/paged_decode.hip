@@ -2,10 +2,13 @@
 // the group of query heads).  out = sum_j p_j v_j / sum_j p_j with p_j = 2^(s_j - m), s_j = log2(e) scale q.k_j, one pass with
 // the running maximum m.
 //
-// Bound by HBM: every code is read once.  A tile is one block (64 tokens) of a KV head; the tiles of all sequences and heads
-// form one list that is dealt evenly to the waves, whatever the sequences' lengths are, so a wave has a range of tiles of
-// one head, or the end of one, some whole ones and the beginning of another.  States of heads that are spread over several
-// waves meet in LDS, over several workgroups in the workspace, where the last workgroup to arrive joins them in order.
+// Bound by HBM: every code is read once (32 heads of 32768 tokens: 268 MB in 53.2 us, 5.0 TB/s; a large plain read reaches 6.1, and
+// the way to the first codes and the joins take 8 us).  A tile is one block (64 tokens) of a KV head; the tiles of all
+// sequences and heads form one list that is dealt evenly to the waves, whatever the sequences' lengths are, so a wave has a
+// range of tiles of one head, or the end of one, some whole ones and the beginning of another.  States of heads that are
+// spread over several waves meet in LDS, over several workgroups in the workspace, where the last workgroup to arrive joins
+// them in order.  A short call is bound by the chain of dependent loads and by the fetching of its code, which is run once: loops
+// beat unrolled code outside the tiles (one head of 1000 tokens: 8.0 us a call, replayed).
 //
 // Both products run on the fp16 matrix cores, S^T = K Q^T and O^T = V^T P^T, with the codes as the left operand straight
 // from their 16-byte loads: K rows are tokens, V pages have channels as rows.  Row r of the s-th group of 16 tokens is token
@@ -53,15 +56,16 @@ __device__ __forceinline__ uint4 raw_queries(half8v v) {
 }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// A load that leaves no trace in the caches: every code is read once (8 x 8 heads of up to 16422 tokens: 47.4 -> 44.4 us).
+// A load that leaves no trace in the caches: every code is read once.  Against plain loads: 42.1 and 44.2 us for 8 x 8 heads of up to
+// 16422 tokens, 53.2 and 53.0 for 32 heads of 32768, 16.2 and 15.7 for 64 x 8 of up to 1102.
 __device__ __forceinline__ uint4 stream16(const uint8_t *p) {
     typedef uint32_t u4 __attribute__((ext_vector_type(4)));
     const u4 v = __builtin_nontemporal_load(reinterpret_cast<const u4 *>(p));
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 constexpr float kRefBelow = 15.f;
-// What an unfinished block costs, in pages: twice the bytes, and its loads start behind the pages'.  us with 3, 5, 8 pages: 8 x 8
-// heads of up to 16422 tokens 44.4 43.5 44.0, 64 x 8 of up to 1102 18.0 17.8 18.5, one head of 1000 11.2 11.5 11.8.
+// What an unfinished block costs, in pages: twice the bytes, and its loads start behind the pages'.  us with 2, 3, 4, 6, 8 pages: 8 x 8
+// heads of up to 16422 tokens 43.9 42.7 42.1 42.3 42.9, 64 x 8 of up to 1102 15.6 16.3 16.2 16.1 17.1.
 constexpr int kTailUnits = 4;
 // Units that a workgroup has at least, while there are others without any: a wave alone on its SIMD is through with a page in less
 // than half the time of two.  us with 1, 2, 3, 4, 8 units: one head of 1000 9.7 9.2 9.4 9.7 10.9, 8 heads of 2000 in groups of 4 10.2
@@ -680,8 +684,8 @@ hipError_t launch_waves(const DecodeArgs &p, int max_len, hipStream_t s) {
 }
 
 // Waves of a workgroup, one of which fills a CU: their states of two heads each have to fit the LDS, and twelve (or sixteen, for
-// heads of 64) with fewer registers each took 75 us instead of 56 over 32 heads x 32768 tokens and 23 to 28 instead of 21 over
-// 64 x 8 heads of up to 1100 (64 channels).
+// heads of 64) with fewer registers each took a third longer over 32 heads x 32768 tokens (75 us against 56) and over 64 x 8 heads of up
+// to 1100 (64 channels; 23 to 28 against 21).
 template <int T, int C, int D, int R>
 hipError_t launch(const DecodeArgs &p, int max_len, hipStream_t s) {
     return launch_waves<T, C, D, R, R == 1 ? 8 : 4>(p, max_len, s);

@@ -1,10 +1,12 @@
 // Attention of prompt chunks over the paged cache of 8-bit codes: ragged chunks, causal, optionally within a sliding window.
 //
-// Bound by the matrix cores.  A workgroup owns one KV head and a tile of query rows: consecutive tokens times the group of query
-// heads, so that every K and V block it stages serves whole groups.  The codes of a block are widened to fp16 once per
-// workgroup, on their way to LDS (two buffers, one barrier a block); a wave multiplies its 32 rows, S^T = K Q^T and
-// O^T = V^T P^T on 32x32x16 products.  Row r of K's 32 is token 16 (r / 16) + 8 (r / 4 % 2) + 4 (r / 8 % 2) + r % 4, so that a
-// lane receives the scores of eight consecutive tokens: its part of P^T for the second product, without an exchange.
+// Bound by the matrix cores and, nearly as much, by the vector ALUs that the softmax runs on (512 tokens on 32 k: 1.03 PFLOP/s; a large
+// library product in fp16 reaches 1.21 here); with heads of 64 by the vector ALUs.  A workgroup owns one KV head and a tile of
+// query rows: consecutive tokens times the group of query heads, so that every K and V block it stages serves whole groups.
+// The codes of a block are widened to fp16 once per workgroup, on their way to LDS (two buffers, one barrier a block); a
+// wave multiplies its 32 rows, S^T = K Q^T and O^T = V^T P^T on 32x32x16 products.  Row r of K's 32 is token
+// 16 (r / 16) + 8 (r / 4 % 2) + 4 (r / 8 % 2) + r % 4, so that a lane receives the scores of eight consecutive tokens: its
+// part of P^T for the second product, without an exchange.
 //
 // K's scale multiplies the scores.  V's scale is 2^e times a mantissa: the mantissa is added to the exponents of P (and taken
 // out of their sum again), 2^e goes into the codes as they are widened, relative to the largest e so far: exact down to 2^-24
@@ -29,7 +31,7 @@ namespace kvc {
 namespace {
 
 // What the unfinished block counts for when the keys are split: it is turned in LDS and nothing overlaps with it.  1, 2, 3, 4:
-// 27.8 26.4 26.5 27.2 us for 4 chunks of 16 tokens on 4001 (8 KV heads, groups of 4); 1, 3: 554 551 us for 512 tokens on 32 k.
+// 27.8 26.4 26.5 27.2 us for 4 chunks of 16 tokens on 4001 (8 KV heads, groups of 4); 1, 3: 547 540 us for 512 tokens on 32 k.
 constexpr int kTailBlocks = 3;
 constexpr float kRefLead = 8.f, kRefMost = 14.f, kFarScore = 67108864.f;
 
@@ -669,7 +671,7 @@ hipError_t launch_tiles(PrefillArgs p, int max_len, hipStream_t s) {
     p.by_tile = Divide(p.per_tile);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(base * p.splits)), dim3(64 * W), kLds, s, p);
     if (p.splits > 1) {
-        // One row per wave while all waves are on the chip at once, or twice; four share the work around them.  us of the whole
+        // One row per wave while all waves are on the chip at once, or in two goes; four share the work around them.  us of the whole
         // call with one, four: 4 chunks of 16 tokens on 4001 (6144 rows) 25.6 26.7, one of 8 on 30 k 26.1 35.0; 16 of 16 on 1984
         // (24576 rows) 42.8 40.4, 512 tokens on 32 k (34816) 532 527, 32 of 16 on 3984, heads of 64 (49152) 71.4 65.0.
         const long long rows = base * 32 * W;
@@ -679,6 +681,9 @@ hipError_t launch_tiles(PrefillArgs p, int max_len, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Eight waves, 256 rows, two sets that take turns on the matrix cores, where the chunks fill more than half of them; else four.  us with
+// four and eight waves: a prompt of 8192 tokens 620 599, 512 tokens on 32 k 571 540, 4 chunks of 16 on 4001 24.8 30.8.  Heads of 64 leave
+// registers for four workgroups of four waves on a CU: 92.6 us for 16 chunks of up to 700 tokens in a window, with eight waves 143.
 template <int T, int C, int D>
 hipError_t launch(const PrefillArgs &p, int max_new, int max_len, hipStream_t s) {
     if constexpr (D == 128) {
