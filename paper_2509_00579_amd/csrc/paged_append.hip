@@ -1,8 +1,8 @@
 // Appending to the paged cache of 8-bit codes: rotate, round to 16 bits, and either quantize a block that ends into its page or
 // store the unfinished block's new rows in its tail; the queries of the same tokens are rotated along.
 //
-// Bound by HBM for prompts (16421 tokens of 8 KV and 32 query heads: 379 MB in 75.3 us, 5.0 TB/s, what a large copy reaches) and by the
-// launch for single tokens (one sequence: 2.7 us a call, replayed).  One workgroup of 16 * D / 16 threads owns a block of 64 tokens
+// Bound by HBM for prompts (16421 tokens of 8 KV and 32 query heads: 379 MB in 75.0 us, 5.0 TB/s, what a large copy reaches) and by the
+// launch for single tokens (one sequence: 2.6 us a call, replayed).  One workgroup of 16 * D / 16 threads owns a block of 64 tokens
 // of one KV head: thread (rg, item) holds four consecutive tokens x two chunks of eight channels of K and of V in registers
 // (all of its sixteen 16-byte loads are on their way together), so that the block's largest magnitudes are one reduction
 // and every value is read once.  The two chunks are the partners of the split rotation, so both results of a pair come
@@ -215,21 +215,26 @@ __global__ __launch_bounds__(kRowGroups * D / 16) void paged_append_kernel(Paged
     // which block of which sequence
     int unit = (int)by_heads.of(blockIdx.x);
     const int h = blockIdx.x - unit * g.H;
-    int b, start, fresh, len;  // first new row, new tokens
+    int b, start, fresh, len, tail;  // first new row, new tokens
     bool bad = false;
     if (!n.starts) {
         b = unit;
         unit = 0;
         len = g.lens[b];
+        tail = g.tails[b];
         fresh = len == 0 ? 0 : 1;
         start = b;
         bad = len < 0 || len > g.max_pages * kPBT;
     } else {
         b = -1;
         for (int base = 0; base < g.batch; base += 64) {
-            int blocks = 0;
+            int blocks = 0, s0 = 0, s1 = 0, l = 0, t = 0;
             if (base + lane < g.batch) {
-                const int s0 = n.starts[base + lane], s1 = n.starts[base + lane + 1], l = g.lens[base + lane];
+                s0 = n.starts[base + lane];
+                s1 = n.starts[base + lane + 1];
+                l = g.lens[base + lane];
+                t = g.tails[base + lane];
+                asm volatile("" ::"v"(l), "v"(t));  // all on their way at once
                 if (s0 < 0 || s1 < s0 || s1 > n.n_tokens || l < s1 - s0 || l > g.max_pages * kPBT) {
                     if (blockIdx.x == 0 && tid < 64) flag(g.fault, kFaultLength);
                 } else if (s1 > s0) {
@@ -243,15 +248,16 @@ __global__ __launch_bounds__(kRowGroups * D / 16) void paged_append_kernel(Paged
                 const int at = __builtin_ctzll(past);
                 b = base + at;
                 unit -= __builtin_amdgcn_readlane(before, at);
+                start = __builtin_amdgcn_readlane(s0, at);
+                fresh = __builtin_amdgcn_readlane(s1, at) - start;
+                len = __builtin_amdgcn_readlane(l, at);
+                tail = __builtin_amdgcn_readlane(t, at);
                 if (blockIdx.x) break;  // the first workgroup looks at all sequences
             } else {
                 unit -= __builtin_amdgcn_readlane(before + blocks, 63);
             }
         }
         if (b < 0) return;
-        start = n.starts[b];
-        fresh = n.starts[b + 1] - start;
-        len = g.lens[b];
     }
 
     if (!n.starts && n.q && fresh) {
@@ -283,7 +289,6 @@ __global__ __launch_bounds__(kRowGroups * D / 16) void paged_append_kernel(Paged
         return;
     }
     if (fresh == 0) return;
-    const int tail = g.tails[b];
     if ((unsigned)tail >= (unsigned)g.n_tails) {
         if (tid == 0) flag(g.fault, kFaultTail);
         return;
@@ -291,6 +296,7 @@ __global__ __launch_bounds__(kRowGroups * D / 16) void paged_append_kernel(Paged
     const int past = len - fresh, first = past / kPBT, last = len / kPBT;  // `last`: the unfinished block, if len % 64
     int blk = first + unit;
     if (blk == last && unit) return;  // the workgroup of the first block stores the tail
+    const int page = blk == last ? 0 : g.table[(size_t)b * g.max_pages + blk];  // long before it is needed
     const size_t tail_at = ((size_t)tail * g.H + h) * kPBT * D;
 
     uint32_t kx[4][2][4], vx[4][2][4];
@@ -377,7 +383,6 @@ __global__ __launch_bounds__(kRowGroups * D / 16) void paged_append_kernel(Paged
         const float ak = wide_lo<T>(m), av = wide_hi<T>(m);
         const bool live_k = !nan_k && ak >= kTinyBlock, live_v = av >= kTinyBlock;
         const float ik = live_k ? kMostCode<C> / ak : 0.f, iv = live_v ? kMostCode<C> / av : 0.f;
-        const int page = g.table[(size_t)b * g.max_pages + blk];
         const bool page_ok = (unsigned)page < (unsigned)g.n_pages;
         const size_t tile = ((size_t)page * g.H + h) * kPBT * D;
         if (page_ok) {

@@ -163,7 +163,7 @@ __device__ __forceinline__ void store_rows(uint16_t *out, int half, const RowSta
 
 template <int T, int C, int D, int W>
 __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill_kernel(PrefillArgs p) {
-    constexpr int kPreWaves = W, kPreRows = 32 * W, kPreThreads = 64 * W;
+    constexpr int kPreRows = 32 * W, kPreThreads = 64 * W;
     constexpr int kUnits = kPBT * D / 8, kPieces = (kPBT * D / 16 + kPreThreads - 1) / kPreThreads;  // 16-byte units of a tile; pieces of 16 codes per thread
     extern __shared__ __align__(16) uint4 s_tiles[];  // [2 buffers][K, V][kUnits]
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n = lane & 31, half = lane >> 5;
@@ -683,7 +683,7 @@ hipError_t launch_tiles(PrefillArgs p, int max_len, hipStream_t s) {
 
 // Eight waves, 256 rows, two sets that take turns on the matrix cores, where the chunks fill more than half of them; else four.  us with
 // four and eight waves: a prompt of 8192 tokens 620 599, 512 tokens on 32 k 571 540, 4 chunks of 16 on 4001 24.8 30.8.  Heads of 64 leave
-// registers for four workgroups of four waves on a CU: 92.6 us for 16 chunks of up to 700 tokens in a window, with eight waves 143.
+// registers for four workgroups of four waves on a CU: 91 us for 16 chunks of up to 700 tokens in a window, with two of eight waves 99.
 template <int T, int C, int D>
 hipError_t launch(const PrefillArgs &p, int max_new, int max_len, hipStream_t s) {
     if constexpr (D == 128) {
