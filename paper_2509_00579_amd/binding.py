@@ -397,7 +397,9 @@ class PagedCache:
     allocated here.  Which sequence has which pages and tail, and how long it is, comes with every call: lens [batch], table
     [batch, max_pages] and tails [batch] are int32 CUDA tensors, read on the device.  lens counts the call's own tokens.
     `workspace` is the attention calls' scratch, a cache's own if None; caches whose calls never overlap in time (the layers of
-    a model on one stream) may share one, calls on several streams at a time need one each (new_workspace)."""
+    a model on one stream) may share one, calls on several streams at a time need one each (new_workspace).  What the cache
+    allocated itself may be used on any stream, and the cache let go while calls are still running; the caller's tensors are the
+    caller's to keep."""
 
     def __init__(self, n_kv_heads, n_q_heads, n_pages, n_tails, head_dim=D, dtype=torch.float16, codes="int8", device="cuda:0",
                  storage=None, workspace=None):
@@ -411,8 +413,9 @@ class PagedCache:
         kinds = (("k_codes", (n_pages, n_kv_heads, BT, head_dim), code), ("v_codes", (n_pages, n_kv_heads, head_dim, BT), code),
                  ("scales", (n_pages, n_kv_heads, 2), torch.float32), ("k_tail", (n_tails, n_kv_heads, BT, head_dim), dtype),
                  ("v_tail", (n_tails, n_kv_heads, BT, head_dim), dtype))
+        self._own = []
         if storage is None:
-            storage = [torch.empty(shape, dtype=t, device=self.device) for _, shape, t in kinds]
+            storage = self._own = [torch.empty(shape, dtype=t, device=self.device) for _, shape, t in kinds]
         for (name, shape, t), x in zip(kinds, storage):
             assert x.device == self.device and x.dtype is t and x.is_contiguous() and x.shape == shape, (
                 f"{name} must be a contiguous {t} tensor {shape} on {self.device}")
@@ -422,7 +425,10 @@ class PagedCache:
         self._memory = _PAGED_CACHE.pack(*(x.data_ptr() for x in (*storage, self.fault)))
         self._index = self.device.index
         self._config = {}
+        self._streams = {torch._C._cuda_getCurrentRawStream(self._index)}  # that the allocator knows the cache's own tensors on
         self._workspace = self.new_workspace() if workspace is None else self._scratch(workspace)
+        self._own = [*self._own, self.fault] + ([self._workspace] if workspace is None else [])
+        self._settle()
 
     def _cfg(self, max_pages):
         cfg = self._config.get(max_pages)
@@ -455,7 +461,17 @@ class PagedCache:
     def _on_device(self):
         if torch._C._cuda_getDevice() != self._index:
             raise KvcompError(ERR_INVALID_ARG, f"the current device is not the cache's ({self.device})")
-        return torch._C._cuda_getCurrentRawStream(self._index)
+        stream = torch._C._cuda_getCurrentRawStream(self._index)
+        if stream not in self._streams:
+            for x in self._own:
+                x.record_stream(torch.cuda.current_stream(self.device))
+            self._streams.add(stream)
+        return stream
+
+    def _settle(self):
+        """What was cleared on this stream is used on others."""
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream(self.device).synchronize()
 
     def append(self, k, v, lens, table, tails, starts=None, q=None, q_out=None, rope=None, positions=None):
         """Append k, v [n, n_kv_heads, head_dim]: one token per sequence (starts None: n = batch), or rows starts[b] ..
@@ -496,7 +512,9 @@ class PagedCache:
 
     def new_workspace(self):
         """Scratch of the attention calls, for one of them at a time."""
-        return torch.zeros(self.lib.kvcomp_paged_workspace_bytes(self._cfg(1)), dtype=torch.uint8, device=self.device)
+        workspace = torch.zeros(self.lib.kvcomp_paged_workspace_bytes(self._cfg(1)), dtype=torch.uint8, device=self.device)
+        self._settle()
+        return workspace
 
     def _scratch(self, workspace):
         assert workspace.get_device() == self._index and workspace.dtype is torch.uint8 and workspace.is_contiguous()

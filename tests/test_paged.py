@@ -832,6 +832,25 @@ def test_many_sequences_with_empty_places(gpu):
     w.check()
 
 
+def test_a_cache_let_go_while_another_stream_uses_it(gpu):
+    """Its memory is not handed out again before that stream is through with it."""
+    cache = gpu.PagedCache(2, 4, 64, 2, head_dim=64)
+    n, at = cache._workspace.numel(), cache._workspace.data_ptr()
+    q = torch.zeros((1, 4, 64), dtype=torch.float16, device="cuda:0")
+    seqs = (_i32([0]), _i32([[0, 1]]), _i32([0]))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+        out = cache.attn_decode(q, 0.1, *seqs)
+    del cache
+    others = [torch.empty(n, dtype=torch.uint8, device="cuda:0") for _ in range(2)]
+    busy = not side.query()
+    assert not busy or all(x.data_ptr() != at for x in others)
+    side.synchronize()
+    assert (out == 0).all()
+
+
 def test_the_binding_refuses(gpu):
     cache = gpu.PagedCache(2, 4, 4, 2, head_dim=64)
     seqs = (_i32([1]), _i32([[0, 1]]), _i32([0]))
