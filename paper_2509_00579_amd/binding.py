@@ -367,6 +367,10 @@ class BaselineFp16Attention:
         return out
 
 
+# looked up once: the calls of a step are short
+_current_device, _raw_stream = (getattr(torch._C, n, None) for n in ("_cuda_getDevice", "_cuda_getCurrentRawStream"))
+
+
 class Rope:
     """The position rotation of PagedCache.append: `cos_sin` is a CUDA fp32 tensor [positions, rot_dim], the cosines of the
     rot_dim / 2 pairs and then their sines; interleaved: pairs are neighbouring channels instead of the two halves of the
@@ -404,6 +408,8 @@ class PagedCache:
     def __init__(self, n_kv_heads, n_q_heads, n_pages, n_tails, head_dim=D, dtype=torch.float16, codes="int8", device="cuda:0",
                  storage=None, workspace=None):
         self.lib = load()
+        self._append, self._decode, self._prefill = (self.lib.kvcomp_paged_append, self.lib.kvcomp_paged_attn_decode,
+                                                     self.lib.kvcomp_paged_attn_prefill)
         self.device = torch.device(device)
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
@@ -425,7 +431,7 @@ class PagedCache:
         self._memory = _PAGED_CACHE.pack(*(x.data_ptr() for x in (*storage, self.fault)))
         self._index = self.device.index
         self._config = {}
-        self._streams = {torch._C._cuda_getCurrentRawStream(self._index)}  # that the allocator knows the cache's own tensors on
+        self._streams = {_raw_stream(self._index)}  # that the allocator knows the cache's own tensors on
         self._workspace = self.new_workspace() if workspace is None else self._scratch(workspace)
         self._own = [*self._own, self.fault] + ([self._workspace] if workspace is None else [])
         self._settle()
@@ -454,14 +460,16 @@ class PagedCache:
         """Pointer and token stride of a tensor [n, heads, head_dim] whose tokens may be apart (a slice of a fused projection)."""
         assert x.get_device() == self._index and x.dtype is self.dtype, f"{name} must be {self.dtype} on {self.device}"
         assert x.shape == shape, f"{name}: expected shape {shape}, got {tuple(x.shape)}"
+        if x.is_contiguous():
+            return x.data_ptr(), shape[1] * shape[2]
         s0, s1, s2 = x.stride()
         assert s2 == 1 and (s1 == shape[2] or shape[1] == 1), f"the heads of a token of {name} must be contiguous"
         return x.data_ptr(), s0 if shape[0] > 1 else shape[1] * shape[2]
 
     def _on_device(self):
-        if torch._C._cuda_getDevice() != self._index:
+        if _current_device() != self._index:
             raise KvcompError(ERR_INVALID_ARG, f"the current device is not the cache's ({self.device})")
-        stream = torch._C._cuda_getCurrentRawStream(self._index)
+        stream = _raw_stream(self._index)
         if stream not in self._streams:
             for x in self._own:
                 x.record_stream(torch.cuda.current_stream(self.device))
@@ -505,7 +513,7 @@ class PagedCache:
                 assert positions.shape == (axes, n), f"positions: expected shape {(axes, n)}, got {tuple(positions.shape)}"
                 pp = positions.data_ptr()
         new = _PAGED_NEW.pack(n, sp, kp, vp, ks, vs, qp, op, qs, os_, cp, n_pos, rot, inter, axes, *sections, pp)
-        st = self.lib.kvcomp_paged_append(cfg, self._memory, seqs, new, stream)
+        st = self._append(cfg, self._memory, seqs, new, stream)
         if st:
             _check(st)
         return q_out
@@ -531,8 +539,8 @@ class PagedCache:
         qp, qs = self._rows(q, shape, "q")
         op, os_ = self._rows(out, shape, "out")
         ws = self._workspace if workspace is None else self._scratch(workspace)
-        _check(self.lib.kvcomp_paged_attn_decode(cfg, self._memory, seqs, qp, qs, q_len, float(scale), window,
-                                                 max_len, op, os_, ws.data_ptr(), ws.numel(), stream))
+        _check(self._decode(cfg, self._memory, seqs, qp, qs, q_len, float(scale), window, max_len, op, os_, ws.data_ptr(), ws.numel(),
+                            stream))
         return out
 
     def attn_prefill(self, q, scale, starts, lens, table, tails, max_new=0, max_len=0, window=0, out=None, workspace=None):
@@ -548,8 +556,8 @@ class PagedCache:
         qp, qs = self._rows(q, shape, "q")
         op, os_ = self._rows(out, shape, "out")
         ws = self._workspace if workspace is None else self._scratch(workspace)
-        _check(self.lib.kvcomp_paged_attn_prefill(cfg, self._memory, seqs, qp, qs, sp, n,
-                                                  float(scale), window, max_new, max_len, op, os_, ws.data_ptr(), ws.numel(), stream))
+        _check(self._prefill(cfg, self._memory, seqs, qp, qs, sp, n, float(scale), window, max_new, max_len, op, os_, ws.data_ptr(),
+                             ws.numel(), stream))
         return out
 
     def check(self):
