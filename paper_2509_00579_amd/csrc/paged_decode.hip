@@ -529,7 +529,7 @@ __global__ __launch_bounds__(64 * W) void paged_decode_kernel(DecodeArgs p) {
 
     // Join the parked states of each head; a head that other workgroups have a part of leaves its state in the workspace.
     int open = 0, open_b[2], open_h[2];
-    uint32_t open_begin[2], open_units[2];
+    uint32_t open_from[2], open_parts[2];  // workgroups that the head is spread over
     const int4 of = s_of[min(lane, kSlots - 1)];  // a slot a lane
     uint32_t left = (uint32_t)__builtin_amdgcn_ballot_w64(of.x >= 0 && lane < kSlots);
     while (left) {
@@ -586,8 +586,8 @@ __global__ __launch_bounds__(64 * W) void paged_decode_kernel(DecodeArgs p) {
             const int k = open++ & 1;  // two at most: the one that began before, the one that goes on behind
             open_b[k] = sb;
             open_h[k] = sh;
-            open_begin[k] = begin;
-            open_units[k] = units;
+            open_from[k] = deal.owner(begin);  // here, while the states are on their way
+            open_parts[k] = deal.owner(begin + units - 1) - open_from[k] + 1;
         }
     }
     if (!open) return;
@@ -596,7 +596,7 @@ __global__ __launch_bounds__(64 * W) void paged_decode_kernel(DecodeArgs p) {
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     for (int k = 0; k < open; k++) {
-        const uint32_t from = deal.owner(open_begin[k]), parts = deal.owner(open_begin[k] + open_units[k] - 1) - from + 1;
+        const uint32_t from = open_from[k], parts = open_parts[k];
         if (tid == 0) {
             const uint32_t ticket = __hip_atomic_fetch_add(p.a.tickets + from, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             s_last[k] = ticket == parts - 1;
