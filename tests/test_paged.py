@@ -872,3 +872,44 @@ def test_the_binding_refuses(gpu):
     with pytest.raises(gpu.KvcompError):
         cache.attn_prefill(q, math.nan, _i32([0, 1]), *seqs)
     cache.check()
+
+
+def test_pages_and_tails_far_into_a_large_cache(gpu):
+    """Offsets beyond 2^32 bytes and 2^31 elements: the same bits as at the beginning."""
+    H, G, D = 8, 2, 128
+    gen = torch.Generator().manual_seed(41)
+    k, v = (torch.randn((150, H, D), generator=gen).to(torch.bfloat16).cuda() for _ in range(2))
+    q = torch.randn((150, H * G, D), generator=gen).to(torch.bfloat16).cuda()
+    got = []
+    for pages, tails, first_page, tail in ((2, 1, 0, 0), (70000, 35000, 69998, 34999)):
+        cache = gpu.PagedCache(H, H * G, pages, tails, head_dim=D, dtype=torch.bfloat16)
+        seqs = (_i32([150]), _i32([[first_page + 1, first_page, 0]]), _i32([tail]))
+        cache.append(k, v, *seqs, starts=_i32([0, 150]))
+        chunk = cache.attn_prefill(q, 0.09, _i32([0, 150]), *seqs)
+        one = cache.attn_decode(q[-1:], 0.09, *seqs)
+        kept = [t[first_page:first_page + 2].view(torch.uint8).clone() for t in (cache.k_codes, cache.v_codes, cache.scales)]
+        kept += [t[tail, :, :22].clone() for t in (cache.k_tail, cache.v_tail)]
+        cache.check()
+        got.append([chunk, one, *kept])
+        del cache
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("G", [16, 32])
+def test_decode_the_largest_batch(gpu, G):
+    """4096 sequences at once, the most, against 64 at a time: the same bits, one unfinished block each."""
+    n, D = 4096, 128
+    gen = torch.Generator().manual_seed(42)
+    cache = gpu.PagedCache(1, G, 1, n, head_dim=D)
+    lens, tails, table = (torch.arange(n) % 7), torch.randperm(n, generator=gen), _i32(torch.zeros((n, 1)))
+    starts = _i32(torch.cat([torch.zeros(1, dtype=torch.int64), lens.cumsum(0)]))
+    lens, tails = _i32(lens), _i32(tails)
+    k, v = (torch.randn((int(starts[-1]), 1, D), generator=gen).half().cuda() for _ in range(2))
+    cache.append(k, v, lens, table, tails, starts=starts)
+    q = torch.randn((n, G, D), generator=gen).half().cuda()
+    got = cache.attn_decode(q, 0.09, lens, table, tails)
+    for at in range(0, n, 64):
+        part = slice(at, at + 64)
+        assert torch.equal(got[part], cache.attn_decode(q[part], 0.09, lens[part], table[part], tails[part])), at
+    assert (got[::7] == 0).all() and not (got[1::7] == 0).all()
+    cache.check()
