@@ -346,7 +346,8 @@ kvcomp_status kvcomp_paged_attn_decode(const kvcomp_paged_config *cfg, const kvc
  * row at that position sees.  d_q, d_out: DEVICE [n_tokens][n_q_heads][head_dim], as above; rows of d_out outside every sequence's
  * range, and those of a sequence whose starts do not fit into n_tokens, are left as they were.  max_new, max_len: the most new
  * tokens and the longest length as far as the caller knows (0: no idea); they shape the launch only.  One kernel, and a
- * second one where few rows over long sequences make it split the keys.  Errors: INVALID_ARG, CAPACITY, HIP. */
+ * second one where few rows over long sequences make it split the keys.  bf16: values of a whole block whose scale is below 2^-91
+ * of another's of the same sequence may count as zero.  Errors: INVALID_ARG, CAPACITY, HIP. */
 kvcomp_status kvcomp_paged_attn_prefill(const kvcomp_paged_config *cfg, const kvcomp_paged_cache *cache,
                                         const kvcomp_paged_batch *seqs, const void *d_q, size_t q_stride, const void *d_starts,
                                         int n_tokens, float scale, int window, int max_new, int max_len, void *d_out,

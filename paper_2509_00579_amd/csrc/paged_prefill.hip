@@ -9,9 +9,10 @@
 // part of P^T for the second product, without an exchange.
 //
 // K's scale multiplies the scores.  V's scale is 2^e times a mantissa: the mantissa is added to the exponents of P (and taken
-// out of their sum again), 2^e goes into the codes as they are widened, relative to the largest e so far: exact down to 2^-24
-// of it (int8) or 2^-15 (e4m3), off by 2^-25 of the largest scale below that.  So a tile's product adds to the output's
-// accumulators as it is.  P is rounded to fp16 (11 bits, relative to each weight: the reference leaves 2^8 to 2^14 above
+// out of their sum again), 2^e goes into the codes as they are widened, relative to the accumulators' unit, so that a block's
+// product adds to them as it is.  The unit is the largest e so far, until a block lies so far below that fp16 could not hold its
+// codes: then the unit comes down to the block, since the larger ones may be hidden from a row or have no weight in it.  All
+// this is exact, down to 2^-91 of the largest scale that the workgroup has met; V below that counts as zero.  P is rounded to fp16 (11 bits, relative to each weight: the reference leaves 2^8 to 2^14 above
 // one, so weights down to 2^-22 of a row's largest keep all of them), and the sum of the weights is taken from the rounded ones.
 // The exponent is one fused product of the score's factors minus the reference, which was rounded: all weights of a row are off
 // by one common factor, which the division takes out as long as it is neither 0 nor infinite; from scores of 2^26 on it
@@ -34,6 +35,29 @@ namespace {
 // 27.8 26.4 26.5 27.2 us for 4 chunks of 16 tokens on 4001 (8 KV heads, groups of 4); 1, 3: 547 540 us for 512 tokens on 32 k.
 constexpr int kTailBlocks = 3;
 constexpr float kRefLead = 8.f, kRefMost = 14.f, kFarScore = 67108864.f;
+constexpr int kNoExponent = -10000;  // of a scale of zero
+
+// The unit 2^e of the output's accumulators while blocks with V scales of other exponents go by.
+template <int C>
+struct VUnit {
+    // fp16's smallest step is 2^-24 and the smallest code 1 (int8) or 2^-9 (e4m3).
+    static constexpr int kExactBelow = C == kI8 ? 24 : 15;
+    // How far the unit may lie below the largest: 2^26 keys with weights of 2^15 and codes of 2^9 stay within binary32.
+    static constexpr int kDeepest = 76;
+    int e = kNoExponent, largest = kNoExponent;
+    __device__ __forceinline__ bool fits(int block) const { return (uint32_t)(e - block) <= (uint32_t)kExactBelow; }
+    // A block with exponent `block` comes next; returns what that adds to e.
+    __device__ __forceinline__ int next(int block) {
+        if (__builtin_expect(fits(block), 1)) return 0;
+        const int was = e;
+        if (block > e) e = block;
+        else if (block != kNoExponent) e = max(block, largest - kDeepest);
+        largest = max(largest, e);
+        return e - was;
+    }
+    // What the block's codes are widened with.
+    __device__ __forceinline__ float factor(int block) const { return fits(block) ? __uint_as_float((uint32_t)(block - e + 127) << 23) : 0.f; }
+};
 
 struct PrefillArgs {
     PagedGeo g;
@@ -224,7 +248,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         for (int i = 0; i < 16; i++) st.o[c][i] = 0.f;
     st.ref = -INFINITY;
     st.sum = 0.f;
-    int e_ref = -10000;  // the accumulators are in units of 2^e_ref
+    VUnit<C> unit_v;  // of st.o
 
     const int token_row = 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);  // of K's 32, see above
     // the last key that this wave's rows see, and the first row's
@@ -344,7 +368,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
     };
 
     // Page numbers and scales of 64 blocks, a block a lane; V's as its exponent, log2 of its mantissa and what takes that out again.
-    int known = t0, known_page = 0, known_e = -127;
+    int known = t0, known_page = 0, known_e = kNoExponent;
     float known_k = 0.f, known_mant = 0.f, known_inv = 1.f;
     auto learn_pages = [&](int t, int page) __attribute__((always_inline)) {
         known = t;
@@ -358,13 +382,12 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
     auto learn_scales = [&](float2 sc) __attribute__((always_inline)) {
         known_k = sc.x;
         const bool any = sc.y > 0.f;
-        known_e = any ? ilogbf(sc.y) : -127;
+        known_e = any ? ilogbf(sc.y) : kNoExponent;
         known_mant = any ? __builtin_amdgcn_logf(ldexpf(sc.y, -known_e)) : 0.f;
         known_inv = __builtin_amdgcn_exp2f(-known_mant);
     };
     auto e_of = [&](int t) { return __builtin_amdgcn_readlane(known_e, t - known); };
     auto power_of_2 = [&](int e) { return __uint_as_float((uint32_t)max(e + 127, 0) << 23); };  // 0 below the normal range
-    auto to_larger = [&](int e) { return power_of_2(min(e_ref - e, 0)); };
 
     // Two halves of the workgroup's waves, one of each on every SIMD, take turns: while one multiplies (block t's weights with V,
     // then its queries with block t + 1's K), the other weighs its scores and widens its share of the codes of a later block.
@@ -373,7 +396,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
     constexpr int kTilePieces = kPBT * D / 16;
     const int k_piece = tid, v_piece = kTilePieces < kPreThreads ? (tid + kPreThreads / 2) % kPreThreads : tid;
     uint4 ck[kPieces], cv[kPieces];
-    int e_staged = -10000;
+    VUnit<C> staged;
     // Behind the last block the same is done with it again, into buffers that nobody will read: a branch around it would cost the
     // loop copies of whatever it leaves in registers.
     auto fetch_k = [&](int t, uint4 (&c)[kPieces]) __attribute__((always_inline)) {
@@ -401,8 +424,8 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
     };
     auto stage_v = [&](int t, uint4 *sv) __attribute__((always_inline)) {
         const int e = e_of(min(t, t_pages - 1));
-        e_staged = max(e, e_staged);
-        const float by = e - e_staged < (C == kI8 ? -24 : -100) ? 0.f : power_of_2(e - e_staged);
+        staged.next(e);
+        const float by = staged.factor(e);
 #pragma unroll
         for (int i = 0; i < kPieces; i++) {
             const int piece = v_piece + i * kPreThreads, channel = piece / 4, part = piece % 4 * 2;
@@ -449,9 +472,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         for (int t = t0; t < t_pages; t++) {
             if (t + 4 > known + 64) learn_scales(learn_pages(t, page_of(t)));
             const int mine = (t - t0) & 1;
-            const int e = e_of(t);
-            const float by_e = to_larger(e);
-            e_ref = max(e, e_ref);
+            const float by_e = power_of_2(-unit_v.next(e_of(t)));
             weigh(t, bcast(known_k, t - known), bcast(known_mant, t - known), bcast(known_inv, t - known), by_e, some_hidden(t));
             stage_k(buffer(t + 1 + lead), ck);
             stage_v(t + lead, buffer(t + lead) + kUnits);
@@ -475,9 +496,9 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         const int t = unfinished;
         uint4 *sk = s_tiles, *sv = sk + kUnits;
         if (!kTailAhead) ask_tail();
-        const int e = T == kBF16 ? 24 : 0;
-        const float by_e = to_larger(e);
-        e_ref = max(e, e_ref);
+        const int e_ref = max(unit_v.e, T == kBF16 ? 24 : 0);
+        const float by_e = power_of_2(unit_v.e - e_ref);
+        unit_v.e = e_ref;
         const float v_by = T == kBF16 ? 1.f : power_of_2(-e_ref), w_by = T == kBF16 ? power_of_2(-e_ref) : 1.f;
         __syncthreads();  // the tiles are free
 #pragma unroll
@@ -543,13 +564,13 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(st.sum), __float_as_uint(st.sum), false, false);
         sum = __uint_as_float(both[0]) + __uint_as_float(both[1]);
     }
-    e_ref = max(e_ref, -140);  // still there where nothing was met
+    const int e_ref = max(unit_v.e, -140);  // nothing was met: any
     if (p.splits == 1) {
         if (!live) return;
-        const float f = rt.bad ? __builtin_nanf("") : sum == 0.f ? 0.f : 1.f / sum, unit_v = ldexpf(1.f, e_ref);
+        const float f = rt.bad ? __builtin_nanf("") : sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
         for (int c = 0; c < D / 32; c++) st.o[c] *= f;  // first: with their unit they could be too large
-        store_rows<T, D>(p.a.out + (size_t)(rt.start + place) * p.a.out_stride + (size_t)head * D, half, st, unit_v);
+        store_rows<T, D>(p.a.out + (size_t)(rt.start + place) * p.a.out_stride + (size_t)head * D, half, st, ldexpf(1.f, e_ref));
         return;
     }
     float *part = p.a.partials + (((size_t)(unit * p.g.H + h) * p.splits + split) * kPreRows + r) * partial_pitch(D);

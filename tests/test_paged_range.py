@@ -1,0 +1,103 @@
+"""Prefill attention over the paged cache where values of very different size meet, against the model in 64 bits: what a row does not
+see or gives no weight must not cost the values that it does see their bits."""
+import math
+
+import pytest
+import torch
+
+import paged_model as M
+import test_paged as P
+
+pytestmark = pytest.mark.gpu
+gpu = P.gpu
+
+
+def _expected(w, rows, window, scale, q, lens=None):
+    """Outputs in 64 bits and what each may be off by, the last rows[b] tokens of every sequence, one after the other.
+
+    Once eps / 2 of the value (or half the type's smallest step).  A weight: 2 * 136 * 2^-24 of the sum of magnitudes behind the
+    score (128 products, eight factors, numerator and denominator), 2 * 2^-11 for its fp16 rounding and the sum's, 2 * 64 * 2^-24 for
+    sums with a rescaling per block.  A weight below fp16's normal range is off by half of fp16's smallest step, 2^-25, with the
+    row's largest at 2^8 or more: 2^-33 of the sum of the weights; but where it rounds to nothing, by itself."""
+    now, out, tol, at = M.Snapshot(w.cache), [], [], 0
+    lens = w.lens if lens is None else lens
+    eps, G = torch.finfo(w.dtype).eps / 2, w.Hq // w.H
+    for b, n in enumerate(rows):
+        k, v = now.held(w.table[b], w.tails[b], lens[b])
+        pos, j = torch.arange(lens[b] - n, lens[b])[:, None], torch.arange(lens[b])
+        seen = j <= pos
+        if window:
+            seen &= j > pos - window
+        for g in range(w.Hq):
+            x = q[at:at + n, g].double()
+            kk, vv = k[:, g // G], v[:, g // G]
+            s = torch.where(seen, x @ kk.t() * scale, torch.full((), -math.inf, dtype=torch.float64))
+            spread = torch.where(seen, x.abs() @ kk.abs().t() * abs(scale), torch.zeros((), dtype=torch.float64)).amax(1, keepdim=True)
+            p = torch.softmax(s, dim=-1)
+            o, size, faint = p @ vv, p @ vv.abs(), p.clamp(max=2.0 ** -33) @ vv.abs()
+            share = 2 * 136 * 2.0 ** -24 * spread + 2 * 2.0 ** -11 + 2 * 64 * 2.0 ** -24
+            off = share * size + faint
+            out.append(o)
+            tol.append(off + eps * (o.abs() + off) + (2.0 ** -25 if w.dtype is torch.float16 else 2.0 ** -134))
+        at += n
+    heads = lambda x: torch.cat([torch.stack(x[i:i + w.Hq], dim=1) for i in range(0, len(x), w.Hq)])  # noqa: E731
+    return heads(out), heads(tol)
+
+
+def _check(w, rows, q, window=0, scale=None, **kw):
+    scale = 1 / math.sqrt(w.D) if scale is None else scale
+    got = w.cache.attn_prefill(q.cuda(), scale, P._starts(rows), P._i32(w.lens), w.d_table, w.d_tails, window=window, **kw).cpu().double()
+    want, tol = _expected(w, rows, window, scale, q)
+    err = (got - want).abs()
+    assert bool((err <= tol).all()), (float((err - tol).max()), float((err / tol).max()))
+    return got
+
+
+def _sided(w, counts, small, sizes, turned):
+    """Tokens whose keys point along a direction u where small(b, place) says so, away from it elsewhere, and whose values are sizes[0]
+    times as large there, sizes[1] times elsewhere; queries along u, those of every `turned`-th token away from it."""
+    n = sum(counts)
+    k, v, q = w.rand(n, w.H, w.D), w.rand(n, w.H, w.D), w.rand(n, w.Hq, w.D)
+    u = torch.where(w.rand(w.D) > 0, 1.0, -1.0)
+    side = torch.tensor([bool(small(b, i)) for b, c in enumerate(counts) for i in range(c)])
+    k = 0.5 * k + 8 * u * torch.where(side, 1.0, -1.0)[:, None, None]
+    v = v * torch.where(side, sizes[0], sizes[1])[:, None, None]
+    q = u + 0.1 * q
+    q[::turned] *= -1
+    return k.to(w.dtype), v.to(w.dtype), q.to(w.dtype)
+
+
+SIZES = {torch.float16: [(2.0 ** -13, 2.0 ** 13)], torch.bfloat16: [(2.0 ** -13, 2.0 ** 13), (2.0 ** -30, 1.0), (2.0 ** -30, 2.0 ** 60)]}
+
+
+@pytest.mark.parametrize("H", [1, 64], ids=["split keys", "one workgroup for all keys"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype,codes", P.TYPES, ids=P.IDS)
+def test_the_weight_lies_on_pages_of_small_values(gpu, dtype, codes, D, H):
+    """Pages whose V scales are 2^26 and more apart, the larger ones first, between and last; keys give them no weight, or all."""
+    for sizes in SIZES[dtype]:
+        w = P.World(gpu, 3, H, 2 if H == 1 else 1, D, dtype, codes, 5, seed=D)
+        counts = [320, 256, 192]
+        large = {0: (0, 3), 1: (1, 2), 2: (2,)}
+        k, v, q = _sided(w, counts, lambda b, i: i // 64 not in large[b], sizes, 5)
+        w.append(counts, k, v)
+        _check(w, counts, q)
+        _check(w, counts, q, max_new=1)  # the other shape of the launch
+        w.check()
+
+
+@pytest.mark.parametrize("H", [1, 64], ids=["split keys", "one workgroup for all keys"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype,codes", P.TYPES, ids=P.IDS)
+def test_large_values_that_the_window_hides(gpu, dtype, codes, D, H):
+    """The first block's values are 2^26 times the others'; the rows behind the window do not see them, the tile's first rows do."""
+    w = P.World(gpu, 2, H, 1, D, dtype, codes, 6, seed=D + 1)
+    counts = [384, 320]
+    k, v, q = w.tokens(sum(counts))
+    v = v.double() * 2.0 ** -13
+    for at in (0, 384):
+        v[at:at + 64] *= 2.0 ** 26
+    w.append(counts, k, v.to(dtype))
+    _check(w, counts, q, window=64)
+    _check(w, counts, q, window=100, max_new=1)
+    w.check()
