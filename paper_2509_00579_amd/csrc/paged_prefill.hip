@@ -496,8 +496,13 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         const int t = unfinished;
         uint4 *sk = s_tiles, *sv = sk + kUnits;
         if (!kTailAhead) ask_tail();
-        const int e_ref = max(unit_v.e, T == kBF16 ? 24 : 0);
-        const float by_e = power_of_2(unit_v.e - e_ref);
+        const int e_ref = T == kBF16 ? max(24, unit_v.largest - VUnit<C>::kDeepest) : max(unit_v.e, 0);
+        int up = unit_v.e - e_ref;
+        if (up < -100) {  // in two steps: the pages' values are there still, though 2^up may be none
+            rescale(power_of_2(-100));
+            up += 100;
+        }
+        const float by_e = power_of_2(up);
         unit_v.e = e_ref;
         const float v_by = T == kBF16 ? 1.f : power_of_2(-e_ref), w_by = T == kBF16 ? power_of_2(-e_ref) : 1.f;
         __syncthreads();  // the tiles are free

@@ -101,3 +101,28 @@ def test_large_values_that_the_window_hides(gpu, dtype, codes, D, H):
     _check(w, counts, q, window=64)
     _check(w, counts, q, window=100, max_new=1)
     w.check()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("codes", ["int8", "e4m3"])
+def test_the_smallest_values_beside_an_unfinished_block(gpu, codes, D):
+    """bf16 values around 2^-98, with and without an unfinished block: its unit is far above theirs."""
+    for rest in (0, 22):
+        w = P.World(gpu, 2, 64, 1, D, torch.bfloat16, codes, 6, seed=D + rest)
+        counts = [320 + rest, 256 + rest]
+        k, v, q = w.tokens(sum(counts))
+        w.append(counts, k, (v.double() * 2.0 ** -98).to(torch.bfloat16))
+        _check(w, counts, q)
+        w.check()
+
+
+@pytest.mark.parametrize("codes", ["int8", "e4m3"])
+def test_values_of_all_sizes_before_an_unfinished_block(gpu, codes):
+    """bf16 pages of 2^110 that have no weight, in an unfinished block's workgroup whose values are small, and the other way round."""
+    for sizes in ((2.0 ** -20, 2.0 ** 110), (2.0 ** 110, 2.0 ** -20)):
+        w = P.World(gpu, 2, 64, 1, 64, torch.bfloat16, codes, 4, seed=7)
+        counts = [150, 90]
+        k, v, q = _sided(w, counts, lambda b, i: i // 64 == counts[b] // 64, sizes, 5)
+        w.append(counts, k, v)
+        _check(w, counts, q)
+        w.check()
