@@ -629,10 +629,14 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(PrefillArgs
 #pragma unroll
     for (int i = 0; i < kJoinRows; i++) {
         const float m = state[i].x, l = state[i].y, e = state[i].z;
-        const float top = wave_max(m), e_top = wave_max(e);
-        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-        const float sum = wave_sum(m == -INFINITY ? (l != l ? l : 0.f) : l * f);  // a split that met nothing takes no part
-        w[i] = f * __builtin_amdgcn_exp2f(e - e_top);
+        const bool met = m != -INFINITY;  // a split that met nothing takes no part
+        const float top = wave_max(m);
+        const float f = met ? __builtin_amdgcn_exp2f(m - top) : 0.f;
+        const float sum = wave_sum(met ? l * f : l != l ? l : 0.f);
+        // The output's unit is that of the split that counts most, with its weight taken in: one with large values that the row
+        // gave next to no weight may not push the others' out of binary32.
+        const float e_top = wave_max(met ? e + ceilf(fmaxf(m - top, -1000.f)) : -2000.f);
+        w[i] = ldexpf(f, (int)(e - e_top));
         by[i] = sum == 0.f ? 0.f : 1.f / sum;
         unit_v[i] = ldexpf(1.f, (int)e_top);
     }

@@ -126,3 +126,22 @@ def test_values_of_all_sizes_before_an_unfinished_block(gpu, codes):
         w.append(counts, k, v)
         _check(w, counts, q)
         w.check()
+
+
+@pytest.mark.parametrize("dtype,codes", P.TYPES[2:], ids=P.IDS[2:])
+def test_split_keys_with_values_of_all_sizes(gpu, dtype, codes):
+    """Few rows over a long past, whose splits are in units 2^120 and more apart: all keys small beside an unfinished block, and pages of
+    2^110 without weight before it."""
+    for D, rest in ((64, 22), (128, 22), (128, 0)):
+        w = P.World(gpu, 2, 1, 2, D, dtype, codes, 64, seed=D)
+        counts = [64 * 61 + rest, 64 * 20 + rest]
+        k, v, q = w.tokens(sum(counts))
+        w.append(counts, k, (v.double() * 2.0 ** -98.5).to(dtype))
+        _check(w, [3, 5], q[:8])
+        w.check()
+    w = P.World(gpu, 2, 1, 2, 64, dtype, codes, 64, seed=6)
+    counts = [64 * 61 + 30, 64 * 20 + 10]
+    k, v, q = _sided(w, counts, lambda b, i: i // 64 == counts[b] // 64, (2.0 ** -40, 2.0 ** 110), 100000)
+    w.append(counts, k, v)
+    _check(w, [3, 5], q[1:9])
+    w.check()
