@@ -491,12 +491,12 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         ready_queries();
     }
     if (t_pages < t1) {
-        // The block that is still in 16 bits, on products of its own type: K as it is, V turned.  fp16: V counts as scaled by one; bf16: the
-        // accumulators change to a unit that no sum of its values overflows, and the weights are taken to it in two parts.
+        // The block that is still in 16 bits, on products of its own type: K as it is, V turned.  fp16: the accumulators change to units of
+        // one; bf16: to a unit that no sum of its values overflows, and the weights are taken to it in two parts.
         const int t = unfinished;
         uint4 *sk = s_tiles, *sv = sk + kUnits;
         if (!kTailAhead) ask_tail();
-        const int e_ref = T == kBF16 ? max(24, unit_v.largest - VUnit<C>::kDeepest) : max(unit_v.e, 0);
+        const int e_ref = T == kBF16 ? max(24, unit_v.largest - VUnit<C>::kDeepest) : 0;
         int up = unit_v.e - e_ref;
         if (up < -100) {  // in two steps: the pages' values are there still, though 2^up may be none
             rescale(power_of_2(-100));
@@ -504,7 +504,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
         }
         const float by_e = power_of_2(up);
         unit_v.e = e_ref;
-        const float v_by = T == kBF16 ? 1.f : power_of_2(-e_ref), w_by = T == kBF16 ? power_of_2(-e_ref) : 1.f;
+        const float w_by = power_of_2(-e_ref);
         __syncthreads();  // the tiles are free
 #pragma unroll
         for (int i = 0; i < kMine; i++) {
@@ -514,9 +514,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
 #pragma unroll
             for (int c = 0; c < 8; c++) {
                 const uint32_t x = c & 1 ? w[c >> 1] >> 16 : w[c >> 1] & 0xffffu;
-                uint16_t *to = reinterpret_cast<uint16_t *>(sv + v_unit(8 * chunk + c, row >> 3)) + (row & 7);
-                if constexpr (T == kBF16) *to = (uint16_t)x;
-                else *to = __builtin_bit_cast(uint16_t, (_Float16)((float)__builtin_bit_cast(_Float16, (uint16_t)x) * v_by));
+                reinterpret_cast<uint16_t *>(sv + v_unit(8 * chunk + c, row >> 3))[row & 7] = (uint16_t)x;
             }
         }
         __syncthreads();

@@ -145,3 +145,16 @@ def test_split_keys_with_values_of_all_sizes(gpu, dtype, codes):
     w.append(counts, k, v)
     _check(w, [3, 5], q[1:9])
     w.check()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("codes", ["int8", "e4m3"])
+def test_small_values_of_an_unfinished_block_behind_large_ones(gpu, codes, D):
+    """fp16 values near the type's smallest step in the unfinished block, 2^15 in the pages, which the window or the keys leave no weight."""
+    for window in (0, 8):
+        w = P.World(gpu, 2, 64, 1, D, torch.float16, codes, 5, seed=D + window)
+        counts = [64 * 4 + 40, 64 * 2 + 60]
+        k, v, q = _sided(w, counts, lambda b, i: i // 64 == counts[b] // 64, (2.0 ** -20, 2.0 ** 13), 5)
+        w.append(counts, k, v)
+        _check(w, counts, q, window=window)
+        w.check()
