@@ -331,7 +331,8 @@ size_t kvcomp_paged_workspace_bytes(const kvcomp_paged_config *cfg);
 /* Decode attention, q_len rows per sequence (1, or a few drafted tokens; q_len * n_q_heads / n_kv_heads <= 32): row i of
  * sequence b is d_q row b * q_len + i, stands at position lens[b] - q_len + i and sees the keys at positions up to its own
  * and, with window > 0, above its own minus window.  out = softmax(scale * q.K^T) . V over those, sums in binary32, one
- * rounding to the 16-bit type; a row that sees nothing is zero.  d_q, d_out: DEVICE [batch * q_len][n_q_heads][head_dim],
+ * rounding to the 16-bit type; a row that sees nothing is zero.  A score that binary32 holds as -Inf only takes no part, +Inf
+ * or NaN makes the row NaN.  d_q, d_out: DEVICE [batch * q_len][n_q_heads][head_dim],
  * 16-byte aligned, strides in elements between rows, multiples of 8; the two have no row in common (but may be slices of
  * one buffer's rows).  max_len: the longest length as far as the caller knows (0: max_pages * 64); it sizes the launch only.
  * batch <= 4096.

@@ -321,7 +321,7 @@ __global__ __launch_bounds__(64 * W, workgroups_per_cu(D, W)) void paged_prefill
             st.sum *= alpha;
             rescale(alpha * by_e);
         }
-        const float ref = sees ? st.ref : 0.f;  // anything finite: all scores are -Inf
+        const float ref = fmaxf(st.ref, kLowestRef);  // nothing met yet but hidden keys and scores of -Inf: their weights are zero
         float off = mant - ref;
         if (__builtin_amdgcn_ballot_w64(sees && fabsf(mx) > kFarScore) != 0) {  // see above
 #pragma unroll

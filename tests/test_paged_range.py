@@ -158,3 +158,50 @@ def test_small_values_of_an_unfinished_block_behind_large_ones(gpu, codes, D):
         w.append(counts, k, v)
         _check(w, counts, q, window=window)
         w.check()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("codes", ["int8", "e4m3"])
+def test_scores_of_minus_infinity(gpu, codes, D):
+    """bf16 scores below binary32's range take no part, whether they come first or last; a row with no others is zero; one above it makes
+    the row NaN.  The same from both calls."""
+    for H in (1, 64):
+        w = P.World(gpu, 3, H, 1, D, torch.bfloat16, codes, 4, seed=D)
+        counts = [64 + 64 + 30, 128 + 20, 100]
+        k, v, _ = w.tokens(sum(counts))
+        q = (1 + w.rand(sum(counts), H, D).abs()).to(torch.bfloat16) * 1e20
+        k = (k.double() * 1e-20).to(torch.bfloat16)
+        far = torch.zeros(sum(counts), dtype=torch.bool)
+        far[:64] = True             # the first block
+        far[158 + 128:158 + 148] = True   # an unfinished one
+        far[306:] = True            # all
+        k[far] = -1e20
+        w.append(counts, k, v)
+        lens, args = P._i32(w.lens), (w.d_table, w.d_tails)
+        got = w.cache.attn_prefill(q.cuda(), 0.1, P._starts(counts), lens, *args).cpu().double()
+        assert not got[:64].any() and not got[306:].any()
+        # the rows that see others too: as if the far ones were not there
+        now = M.Snapshot(w.cache)
+        for b, first, last in ((0, 64, 158), (1, 158, 306)):
+            kk, vv = now.held(w.table[b], w.tails[b], counts[b])
+            at = 158 * b
+            j = torch.arange(counts[b])
+            for i in range(first, last):
+                seen = (j <= i - at) & ~far[at:at + counts[b]]
+                s = torch.where(seen[:, None], (q[i].double() * kk).sum(-1) * 0.1, torch.full((), -math.inf, dtype=torch.float64))
+                spread = torch.where(seen[:, None], (q[i].double() * kk).abs().sum(-1) * 0.1, torch.zeros((), dtype=torch.float64)).amax(0)
+                p = torch.softmax(s, dim=0)
+                want, size = (p[..., None] * vv).sum(0), (p[..., None] * vv.abs()).sum(0)
+                faint = (p.clamp(max=2.0 ** -33)[..., None] * vv.abs()).sum(0)
+                share = 2 * 136 * 2.0 ** -24 * spread[:, None] + 2 * 2.0 ** -11 + 2 * 64 * 2.0 ** -24
+                off = share * size + faint
+                assert bool(((got[i] - want).abs() <= off + 2.0 ** -8 * (want.abs() + off)).all()), (b, i)
+        one = w.cache.attn_decode(q[[157, 305, 405]].cuda(), 0.1, lens, *args).cpu().double()
+        few = w.cache.attn_prefill(q[[157, 305, 405]].cuda(), 0.1, P._i32([0, 1, 2, 3]), lens, *args, max_new=1).cpu().double()
+        assert not one[2].any() and not few[2].any()
+        # against the chunk's: a rounding to bf16 on either side, and two of weights to 11 bits, of values up to 5
+        for x in (one, few):
+            assert bool(((x[:2] - got[[157, 305]]).abs() <= 2.0 ** -7 * x[:2].abs() + 2.0 ** -8 * 5).all())
+        up = w.cache.attn_prefill((-q).cuda(), 0.1, P._starts(counts), lens, *args)
+        assert torch.isnan(up[:158]).all() and torch.isnan(up[306:]).all()
+        assert torch.isnan(w.cache.attn_decode((-q[[157, 305, 405]]).cuda(), 0.1, lens, *args)).all()
