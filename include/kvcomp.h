@@ -356,8 +356,9 @@ kvcomp_status kvcomp_paged_attn_prefill(const kvcomp_paged_config *cfg, const kv
 
 /* What kernels flagged since the last check, once, and in this order: a page, tail or position out of range, or lengths or
  * starts that do not fit (STATE: such a sequence's tokens were not stored, its output rows are NaN; a token at a position
- * outside the table counts as one that holds NaN), Inf or NaN in what was appended (NONFINITE).  SYNCHRONISES `stream` and
- * clears the flags. */
+ * outside the table counts as one that holds NaN), Inf or NaN in what was appended (NONFINITE).  The status is that of the first
+ * kind, kvcomp_last_error() names all.  SYNCHRONISES `stream` and clears what it reports; what kernels on other streams flag
+ * meanwhile is left for the next check. */
 kvcomp_status kvcomp_paged_check(const kvcomp_paged_cache *cache, void *stream);
 
 const char *kvcomp_last_error(void);

@@ -1,4 +1,6 @@
 // The C entry points of the paged cache of 8-bit codes: checks of what the host can see, and the launches.
+#include <stdio.h>
+
 #include "api_error.h"
 #include "paged.cuh"
 
@@ -66,6 +68,10 @@ bool overlap(const void *a, size_t a_stride, size_t a_width, const void *b, size
     if (off >= (size_t)(rows - 1) * a_stride + a_width) return false;
     if (rows == 1 || a_stride != b_stride) return true;
     return off % a_stride < a_width || off % a_stride + b_width > a_stride;
+}
+
+__global__ void paged_clear_kernel(uint32_t *word, uint32_t bits) {
+    __hip_atomic_fetch_and(word, ~bits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 }  // namespace
@@ -206,13 +212,23 @@ kvcomp_status kvcomp_paged_check(const kvcomp_paged_cache *cache, void *stream) 
     HIP_TRY(hipMemcpyAsync(&fault, cache->d_fault, sizeof(fault), hipMemcpyDeviceToHost, s));
     HIP_TRY(hipStreamSynchronize(s));
     if (!fault) return KVCOMP_OK;
-    HIP_TRY(hipMemsetAsync(cache->d_fault, 0, sizeof(fault), s));
+    // only what was read: kernels on other streams may have flagged something else since
+    hipLaunchKernelGGL(paged_clear_kernel, dim3(1), dim3(1), 0, s, cache->d_fault, fault);
+    HIP_TRY(hipGetLastError());
     HIP_TRY(hipStreamSynchronize(s));
-    if (fault & kFaultPage) return fail(KVCOMP_ERR_STATE, "a page that was needed is outside the cache");
-    if (fault & kFaultTail) return fail(KVCOMP_ERR_STATE, "a tail that was needed is outside the cache");
-    if (fault & kFaultLength) return fail(KVCOMP_ERR_STATE, "a length or a start does not fit");
-    if (fault & kFaultPosition) return fail(KVCOMP_ERR_STATE, "a position is outside the table of cosines and sines");
-    return fail(KVCOMP_ERR_NONFINITE, "an appended token held Inf or NaN");
+    static const struct {
+        uint32_t bit;
+        const char *text;
+    } kinds[] = {{kFaultPage, "a page that was needed is outside the cache"},
+                 {kFaultTail, "a tail that was needed is outside the cache"},
+                 {kFaultLength, "a length or a start does not fit"},
+                 {kFaultPosition, "a position is outside the table of cosines and sines"},
+                 {kFaultNonfinite, "an appended token held Inf or NaN"}};
+    char text[256] = "";
+    int at = 0;
+    for (const auto &k : kinds)
+        if (fault & k.bit) at += snprintf(text + at, sizeof(text) - at, "%s%s", at ? "; " : "", k.text);
+    return fail(fault & ~kFaultNonfinite ? KVCOMP_ERR_STATE : KVCOMP_ERR_NONFINITE, "%s", text);
 }
 
 }  // extern "C"
