@@ -402,8 +402,8 @@ class PagedCache:
     [batch, max_pages] and tails [batch] are int32 CUDA tensors, read on the device.  lens counts the call's own tokens.
     `workspace` is the attention calls' scratch, a cache's own if None; caches whose calls never overlap in time (the layers of
     a model on one stream) may share one, calls on several streams at a time need one each (new_workspace).  What the cache
-    allocated itself may be used on any stream, and the cache let go while calls are still running; the caller's tensors are the
-    caller's to keep."""
+    allocated itself, new_workspace's tensors too, may be used on any stream, and let go while calls are still running; the
+    caller's tensors are the caller's to keep."""
 
     def __init__(self, n_kv_heads, n_q_heads, n_pages, n_tails, head_dim=D, dtype=torch.float16, codes="int8", device="cuda:0",
                  storage=None, workspace=None):
@@ -432,8 +432,8 @@ class PagedCache:
         self._index = self.device.index
         self._config = {}
         self._streams = {_raw_stream(self._index)}  # that the allocator knows the cache's own tensors on
-        self._workspace = self.new_workspace() if workspace is None else self._scratch(workspace)
-        self._own = [*self._own, self.fault] + ([self._workspace] if workspace is None else [])
+        self._own = [*self._own, self.fault]
+        self._workspace = self._scratch(self.new_workspace() if workspace is None else workspace, _raw_stream(self._index))
         self._settle()
 
     def _cfg(self, max_pages):
@@ -521,11 +521,19 @@ class PagedCache:
     def new_workspace(self):
         """Scratch of the attention calls, for one of them at a time."""
         workspace = torch.zeros(self.lib.kvcomp_paged_workspace_bytes(self._cfg(1)), dtype=torch.uint8, device=self.device)
+        workspace.known_streams = {_raw_stream(self._index)}  # that the allocator knows it on
         self._settle()
         return workspace
 
-    def _scratch(self, workspace):
-        assert workspace.get_device() == self._index and workspace.dtype is torch.uint8 and workspace.is_contiguous()
+    def _scratch(self, workspace, stream):
+        if workspace is None:
+            workspace = self._workspace
+        else:
+            assert workspace.get_device() == self._index and workspace.dtype is torch.uint8 and workspace.is_contiguous()
+        known = getattr(workspace, "known_streams", None)  # None: the caller's own tensor
+        if known is not None and stream not in known:
+            workspace.record_stream(torch.cuda.current_stream(self.device))
+            known.add(stream)
         return workspace
 
     def attn_decode(self, q, scale, lens, table, tails, q_len=1, window=0, max_len=0, out=None, workspace=None):
@@ -538,7 +546,7 @@ class PagedCache:
             out = torch.empty(shape, dtype=self.dtype, device=self.device)
         qp, qs = self._rows(q, shape, "q")
         op, os_ = self._rows(out, shape, "out")
-        ws = self._workspace if workspace is None else self._scratch(workspace)
+        ws = self._scratch(workspace, stream)
         _check(self._decode(cfg, self._memory, seqs, qp, qs, q_len, float(scale), window, max_len, op, os_, ws.data_ptr(), ws.numel(),
                             stream))
         return out
@@ -555,7 +563,7 @@ class PagedCache:
             out = torch.empty(shape, dtype=self.dtype, device=self.device)
         qp, qs = self._rows(q, shape, "q")
         op, os_ = self._rows(out, shape, "out")
-        ws = self._workspace if workspace is None else self._scratch(workspace)
+        ws = self._scratch(workspace, stream)
         _check(self._prefill(cfg, self._memory, seqs, qp, qs, sp, n, float(scale), window, max_new, max_len, op, os_, ws.data_ptr(),
                              ws.numel(), stream))
         return out

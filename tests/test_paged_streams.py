@@ -48,3 +48,31 @@ def test_checks_while_another_stream_flags(gpu):
             side.synchronize()
         assert "a length or a start does not fit" in said and "an appended token held Inf or NaN" in said, i
     w.cache.check()
+
+
+@pytest.mark.parametrize("how", ["new_workspace", "a cache that shares one"])
+def test_a_workspace_let_go_while_another_stream_uses_it(gpu, how):
+    """Its memory is not handed out again before that stream is through with it."""
+    cache = gpu.PagedCache(2, 4, 64, 2, head_dim=64)
+    ws = cache.new_workspace()
+    n, at = ws.numel(), ws.data_ptr()
+    q = torch.zeros((1, 4, 64), dtype=torch.float16, device="cuda:0")
+    seqs = (P._i32([0]), P._i32([[0, 1]]), P._i32([0]))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+        if how == "new_workspace":
+            out = cache.attn_prefill(q, 0.1, P._i32([0, 1]), *seqs, workspace=ws)
+        else:
+            cache = gpu.PagedCache(2, 4, 64, 2, head_dim=64, storage=[cache.k_codes, cache.v_codes, cache.scales, cache.k_tail,
+                                                                      cache.v_tail], workspace=ws)
+            torch.cuda._sleep(200_000_000)  # making a cache waits for the stream
+            out = cache.attn_decode(q, 0.1, *seqs)
+            cache._workspace = None
+    del ws
+    others = [torch.empty(n, dtype=torch.uint8, device="cuda:0") for _ in range(2)]
+    busy = not side.query()
+    assert not busy or all(x.data_ptr() != at for x in others)
+    side.synchronize()
+    assert (out == 0).all()
