@@ -355,8 +355,10 @@ kvcomp_status kvcomp_paged_attn_prefill(const kvcomp_paged_config *cfg, const kv
                                         size_t out_stride, void *d_workspace, size_t workspace_bytes, void *stream);
 
 /* What kernels flagged since the last check, once, and in this order: a page, tail or position out of range, or lengths or
- * starts that do not fit (STATE: such a sequence's tokens were not stored, its output rows are NaN; a token at a position
- * outside the table counts as one that holds NaN), Inf or NaN in what was appended (NONFINITE).  The status is that of the first
+ * starts that do not fit (STATE: attention's rows of such a sequence are NaN, or left as they were where its starts do not fit; an
+ * append leaves its tail as it was and stores at most those of its whole blocks that have a page, so that it can be repeated
+ * with the right table, though not with queries that it has rotated in place; a token at a position outside the table counts as
+ * one that holds NaN), Inf or NaN in what was appended (NONFINITE).  The status is that of the first
  * kind, kvcomp_last_error() names all.  SYNCHRONISES `stream` and clears what it reports; what kernels on other streams flag
  * meanwhile is left for the next check. */
 kvcomp_status kvcomp_paged_check(const kvcomp_paged_cache *cache, void *stream);

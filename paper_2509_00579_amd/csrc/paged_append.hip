@@ -296,7 +296,9 @@ __global__ __launch_bounds__(kRowGroups * D / 16) void paged_append_kernel(Paged
     const int past = len - fresh, first = past / kPBT, last = len / kPBT;  // `last`: the unfinished block, if len % 64
     int blk = first + unit;
     if (blk == last && unit) return;  // the workgroup of the first block stores the tail
-    const int page = blk == last ? 0 : g.table[(size_t)b * g.max_pages + blk];  // long before it is needed
+    const int32_t *pages = g.table + (size_t)b * g.max_pages;
+    const int page = blk == last ? 0 : pages[blk];  // long before it is needed
+    const int page_of_lane = unit == 0 && first + lane < last ? pages[first + lane] : 0;
     const size_t tail_at = ((size_t)tail * g.H + h) * kPBT * D;
 
     uint32_t kx[4][2][4], vx[4][2][4];
@@ -423,8 +425,13 @@ __global__ __launch_bounds__(kRowGroups * D / 16) void paged_append_kernel(Paged
             }
         }
         if (unit == 0 && last * kPBT < len) {
-            fetch(last, 0, len - last * kPBT, false);
-            keep(0, len - last * kPBT);
+            // the tail keeps its old rows where any block of the sequence has no page: then the call can be repeated
+            bool fits = (unsigned)page_of_lane < (unsigned)g.n_pages;
+            for (int i = first + 64 + lane; i < last; i += 64) fits &= (unsigned)pages[i] < (unsigned)g.n_pages;
+            if (__builtin_amdgcn_ballot_w64(!fits) == 0) {
+                fetch(last, 0, len - last * kPBT, false);
+                keep(0, len - last * kPBT);
+            }
         }
     }
     if (odd) flag(g.fault, kFaultNonfinite);
