@@ -2,13 +2,13 @@
 // the group of query heads).  out = sum_j p_j v_j / sum_j p_j with p_j = 2^(s_j - m), s_j = log2(e) scale q.k_j, one pass with
 // the running maximum m.
 //
-// Bound by HBM: every code is read once (32 heads of 32768 tokens: 268 MB in 53.2 us, 5.0 TB/s; a large plain read reaches 6.1, and
-// the way to the first codes and the joins take 8 us).  A tile is one block (64 tokens) of a KV head; the tiles of all
+// Bound by HBM: every code is read once (32 heads of 32768 tokens, 268 MB: 56 us, 4.8 TB/s, where the caches hold none of them; a large
+// plain read reaches 6.1, and the way to the first codes and the joins take 8 us).  A tile is one block (64 tokens) of a KV head; the tiles of all
 // sequences and heads form one list that is dealt evenly to the waves, whatever the sequences' lengths are, so a wave has a
 // range of tiles of one head, or the end of one, some whole ones and the beginning of another.  States of heads that are
 // spread over several waves meet in LDS, over several workgroups in the workspace, where the last workgroup to arrive joins
 // them in order.  A short call is bound by the chain of dependent loads and by the fetching of its code, which is run once: loops
-// beat unrolled code outside the tiles (one head of 1000 tokens: 8.0 us a call, replayed).
+// beat unrolled code outside the tiles (one head of 1000 tokens: 7.6 us a call, replayed).
 //
 // Both products run on the fp16 matrix cores, S^T = K Q^T and O^T = V^T P^T, with the codes as the left operand straight
 // from their 16-byte loads: K rows are tokens, V pages have channels as rows.  Row r of the s-th group of 16 tokens is token
@@ -56,20 +56,18 @@ __device__ __forceinline__ uint4 raw_queries(half8v v) {
 }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// A load that leaves no trace in the caches: every code is read once.  Against plain loads: 42.1 and 44.2 us for 8 x 8 heads of up to
-// 16422 tokens, 53.2 and 53.0 for 32 heads of 32768, 16.2 and 15.7 for 64 x 8 of up to 1102.
-__device__ __forceinline__ uint4 stream16(const uint8_t *p) {
-    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-    const u4 v = __builtin_nontemporal_load(reinterpret_cast<const u4 *>(p));
-    return make_uint4(v[0], v[1], v[2], v[3]);
-}
+// Codes are read once a call, yet by plain loads: where the last-level cache (256 MB) still holds some from the call before, they are
+// faster, and elsewhere about as fast as ones past the caches.  us, past them -> plain, one cache again and again: 32 heads of 32768
+// 56.2 -> 45.4, 8 x 8 heads of up to 16422 43.8 -> 38.5, 64 x 8 of up to 1102 15.3 -> 14.6; six caches in turn: 57.6 -> 56.5, 43.3 ->
+// 45.0, 17.1 -> 15.6.
+__device__ __forceinline__ uint4 load16(const uint8_t *p) { return *reinterpret_cast<const uint4 *>(p); }
 constexpr float kRefBelow = 15.f;
 // What an unfinished block costs, in pages: twice the bytes, and its loads start behind the pages'.  us with 2, 3, 4, 6, 8 pages: 8 x 8
-// heads of up to 16422 tokens 43.9 42.7 42.1 42.3 42.9, 64 x 8 of up to 1102 15.6 16.3 16.2 16.1 17.1.
+// heads of up to 16422 tokens 39.4 38.7 37.8 37.8 36.8, 64 x 8 of up to 1102 14.4 14.9 14.5 14.5 15.2.
 constexpr int kTailUnits = 4;
 // Units that a workgroup has at least, while there are others without any: a wave alone on its SIMD is through with a page in less
-// than half the time of two.  us with 1, 2, 3, 4, 8 units: one head of 1000 9.7 9.2 9.4 9.7 10.9, 8 heads of 2000 in groups of 4 10.2
-// 9.8 10.1 10.5 12.6, one head in a group of 8 of 4000 14.6 11.8 11.4 11.1 12.7, 8 heads of 300 8.8 9.1 9.6 9.7 8.4.
+// than half the time of two.  us with 1, 2, 3, 4, 8 units: one head of 1000 7.6 7.6 7.9 8.0 9.5, 8 heads of 2000 in groups of 4 9.3
+// 8.7 8.5 8.9 10.7, one head in a group of 8 of 4000 13.7 10.7 10.0 9.7 11.6, 8 heads of 300 7.4 7.5 7.6 7.9 7.1.
 constexpr uint32_t kLeastUnits = 2;
 // bf16: the accumulators hold 2^-40 of the sums, so that neither the largest values overflow them (2^15 of a weight, 2^26 keys)
 // nor the largest weight's of anything that a page holds (2^-100 and more) drops below binary32's normal range; the factor
@@ -143,12 +141,12 @@ struct Wave {
 #pragma unroll
         for (int s = 0; s < 4; s++)
 #pragma unroll
-            for (int j = 0; j < KJ; j++) kr[s][j] = stream16(t + token_of(s) * D + 64 * j);
+            for (int j = 0; j < KJ; j++) kr[s][j] = load16(t + token_of(s) * D + 64 * j);
     }
     __device__ __forceinline__ void load_v(int page, int h) {
         const uint8_t *t = p.g.v_codes + ((size_t)page * p.g.H + h) * kPBT * D + 16 * g4;
 #pragma unroll
-        for (int i = 0; i < CT; i++) vr[i] = stream16(t + (CT * n + i) * kPBT);
+        for (int i = 0; i < CT; i++) vr[i] = load16(t + (CT * n + i) * kPBT);
     }
 
     // Scores of tokens base + 16 g4 + j, j < 16, in powers of two; hidden ones are -Inf whatever they were.
@@ -683,9 +681,8 @@ hipError_t launch_waves(const DecodeArgs &p, int max_len, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Waves of a workgroup, one of which fills a CU: their states of two heads each have to fit the LDS, and twelve (or sixteen, for
-// heads of 64) with fewer registers each took a third longer over 32 heads x 32768 tokens (75 us against 56) and over 64 x 8 heads of up
-// to 1100 (64 channels; 23 to 28 against 21).
+// Waves of a workgroup, one of which fills a CU: their states of two heads each have to fit the LDS, and twelve with fewer registers
+// each take a third longer over 32 heads x 32768 tokens (61 us against 46).
 template <int T, int C, int D, int R>
 hipError_t launch(const DecodeArgs &p, int max_len, hipStream_t s) {
     return launch_waves<T, C, D, R, R == 1 ? 8 : 4>(p, max_len, s);
