@@ -323,9 +323,10 @@ typedef struct {        /* the new tokens of one append                         
 kvcomp_status kvcomp_paged_append(const kvcomp_paged_config *cfg, const kvcomp_paged_cache *cache,
                                   const kvcomp_paged_batch *seqs, const kvcomp_paged_new *fresh, void *stream);
 
-/* Device bytes of the attention calls' scratch for `cfg` (0 if it is invalid).  The caller ZERO-FILLS IT ONCE before the first
- * call (it holds tickets, which every launch leaves at zero again).  Two launches that overlap in time, captured ones
- * included, must not share one. */
+/* Device bytes of the attention calls' scratch for `cfg` (0 if it is invalid): 69 MB for heads of 128, 36 MB for 64, whatever the
+ * cache's size, nearly all of it for prefill calls that split the keys.  The caller ZERO-FILLS IT ONCE before the first call (it
+ * holds tickets, which every launch leaves at zero again).  Layers whose calls follow each other share one; two launches that
+ * overlap in time, captured ones included, must not. */
 size_t kvcomp_paged_workspace_bytes(const kvcomp_paged_config *cfg);
 
 /* Decode attention, q_len rows per sequence (1, or a few drafted tokens; q_len * n_q_heads / n_kv_heads <= 32): row i of
@@ -347,7 +348,8 @@ kvcomp_status kvcomp_paged_attn_decode(const kvcomp_paged_config *cfg, const kvc
  * row at that position sees.  d_q, d_out: DEVICE [n_tokens][n_q_heads][head_dim], as above; rows of d_out outside every sequence's
  * range, and those of a sequence whose starts do not fit into n_tokens, are left as they were.  max_new, max_len: the most new
  * tokens and the longest length as far as the caller knows (0: no idea); they shape the launch only.  One kernel, and a
- * second one where few rows over long sequences make it split the keys.  bf16: values of a whole block whose scale is below 2^-91
+ * second one where few rows over long sequences make it split the keys.  The softmax's weights enter the product with V in fp16,
+ * 11 bits of each (decode: 22), and their sum is that of the rounded ones.  bf16: values of a whole block whose scale is below 2^-91
  * of another's of the same sequence may count as zero.  Errors: INVALID_ARG, CAPACITY, HIP. */
 kvcomp_status kvcomp_paged_attn_prefill(const kvcomp_paged_config *cfg, const kvcomp_paged_cache *cache,
                                         const kvcomp_paged_batch *seqs, const void *d_q, size_t q_stride, const void *d_starts,

@@ -1,9 +1,10 @@
 // Appending to the paged cache of 8-bit codes: rotate, round to 16 bits, and either quantize a block that ends into its page or
 // store the unfinished block's new rows in its tail; the queries of the same tokens are rotated along.
 //
-// Bound by HBM for prompts (16421 tokens of 8 KV and 32 query heads: 379 MB in 75.0 us, 5.0 TB/s, what a large copy reaches) and by the
-// launch for single tokens (one sequence: 2.6 us a call, replayed).  One workgroup of 16 * D / 16 threads owns a block of 64 tokens
-// of one KV head: thread (rg, item) holds four consecutive tokens x two chunks of eight channels of K and of V in registers
+// Bound by HBM for prompts (16421 tokens of 8 KV and 32 query heads: 379 MB in 76 us, 5.0 TB/s, what a large copy reaches; 65 to 67
+// where the caches hold some of it) and by the launch for single tokens (one sequence: 2.6 us a call, replayed).  One workgroup of
+// 16 * D / 16 threads owns a block of 64 tokens of one KV head: thread (rg, item) holds four consecutive tokens x two chunks of
+// eight channels of K and of V in registers
 // (all of its sixteen 16-byte loads are on their way together), so that the block's largest magnitudes are one reduction
 // and every value is read once.  The two chunks are the partners of the split rotation, so both results of a pair come
 // from registers.  The four tokens make the bytes of a V channel's word; V leaves through LDS because its page has the
@@ -132,7 +133,7 @@ template <int C>
 constexpr float kMostCode = C == kI8 ? 127.f : 448.f;
 
 constexpr int kRowGroups = 16;   // four tokens each
-// Rows of queries per thread (16421 tokens, 8 KV and 32 query heads, with 1, 2, 4, 8: 80.6 79.3 80 84 us).
+// Rows of queries per thread (16421 tokens, 8 KV and 32 query heads, with 1, 2, 4, 8: 72.3 66.9 67.4 67.6 us).
 constexpr int kQRows = 2;
 constexpr int kVPitch = 17;      // words of a V channel in LDS: 16, and one so that the writers of eight channels hit eight banks
 
@@ -445,8 +446,8 @@ void launch(const PagedGeo &g, PagedNew n, hipStream_t s) {
     const size_t units = n.starts ? (size_t)n.n_tokens / kPBT + 2 * (size_t)g.batch : (size_t)g.batch;
     const size_t most = n.starts && (size_t)n.n_tokens < units ? (size_t)n.n_tokens : units;
     const size_t q_rows = n.starts && n.q ? (size_t)n.n_tokens * g.H * g.G : 0;
-    // rotated queries that the L2s (8 x 4 MiB) cannot keep for the attention behind go past them: 79.3 -> 75.5 us for 134 MB, but
-    // 20.6 -> 21.8 for 19 MB
+    // rotated queries that the L2s (8 x 4 MiB) cannot keep for the attention behind go past them: 78.8 -> 66.9 us for 134 MB (79.5 ->
+    // 76.1 with other tokens every time), but 19.9 -> 20.5 for 19 MB
     n.stream_q = q_rows * D * 2 > (size_t)32 << 20;
     const size_t q_units = (q_rows + kRowGroups * kQRows - 1) / (kRowGroups * kQRows);
     hipLaunchKernelGGL((paged_append_kernel<T, C, D>), dim3((unsigned)(most * g.H + q_units)), dim3(kRowGroups * D / 16), 0, s, g, n,

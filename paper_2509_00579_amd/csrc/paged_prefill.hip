@@ -1,8 +1,8 @@
 // Attention of prompt chunks over the paged cache of 8-bit codes: ragged chunks, causal, optionally within a sliding window.
 //
-// Bound by the matrix cores and, nearly as much, by the vector ALUs that the softmax runs on (512 tokens on 32 k: 1.03 PFLOP/s; a large
-// library product in fp16 reaches 1.21 here); with heads of 64 by the vector ALUs.  A workgroup owns one KV head and a tile of
-// query rows: consecutive tokens times the group of query heads, so that every K and V block it stages serves whole groups.
+// Bound by the matrix cores and, nearly as much, by the vector ALUs that the softmax runs on (512 tokens on 32 k: 0.97 to 1.02
+// PFLOP/s from box to box; a large library product in fp16 reaches 1.21); with heads of 64 by the vector ALUs.  A workgroup owns one KV
+// head and a tile of query rows: consecutive tokens times the group of query heads, so that every K and V block it stages serves whole groups.
 // The codes of a block are widened to fp16 once per workgroup, on their way to LDS (two buffers, one barrier a block); a
 // wave multiplies its 32 rows, S^T = K Q^T and O^T = V^T P^T on 32x32x16 products.  Row r of K's 32 is token
 // 16 (r / 16) + 8 (r / 4 % 2) + 4 (r / 8 % 2) + r % 4, so that a lane receives the scores of eight consecutive tokens: its
@@ -12,11 +12,16 @@
 // out of their sum again), 2^e goes into the codes as they are widened, relative to the accumulators' unit, so that a block's
 // product adds to them as it is.  The unit is the largest e so far, until a block lies so far below that fp16 could not hold its
 // codes: then the unit comes down to the block, since the larger ones may be hidden from a row or have no weight in it.  All
-// this is exact, down to 2^-91 of the largest scale that the workgroup has met; V below that counts as zero.  P is rounded to fp16 (11 bits, relative to each weight: the reference leaves 2^8 to 2^14 above
-// one, so weights down to 2^-22 of a row's largest keep all of them), and the sum of the weights is taken from the rounded ones.
+// this is exact, down to 2^-91 of the largest scale that the workgroup has met; V below that counts as zero.
+//
+// P is rounded to fp16 (11 bits, relative to each weight: the reference leaves 2^8 to 2^14 above one, so weights down to 2^-22 of
+// a row's largest keep all of them), and the sum of the weights is taken from the rounded ones: the second product runs on one
+// operand instead of two, and an output is off by up to 2^-10 of its values' weighted magnitudes (fp16 against 64 bits, the
+// root of the mean square: 2.6e-4 of them, 2.1e-4 with weights in 32 bits).
 // The exponent is one fused product of the score's factors minus the reference, which was rounded: all weights of a row are off
 // by one common factor, which the division takes out as long as it is neither 0 nor infinite; from scores of 2^26 on it
-// could be, and the product is rounded by itself.
+// could be, and the product is rounded by itself.  (With the mantissa's logarithm in it the reference is rounded once more for every
+// block, by 2^-25 of itself, as much as the scores of its size are.)
 // The reference moves only when a score would pass 2^14 above it, which spares most tiles the rescaling of the accumulators.
 //
 // Few rows over a long axis: the keys are split among workgroups, and a second launch joins their states.
@@ -32,7 +37,7 @@ namespace kvc {
 namespace {
 
 // What the unfinished block counts for when the keys are split: it is turned in LDS and nothing overlaps with it.  1, 2, 3, 4:
-// 27.8 26.4 26.5 27.2 us for 4 chunks of 16 tokens on 4001 (8 KV heads, groups of 4); 1, 3: 547 540 us for 512 tokens on 32 k.
+// 27.0 25.2 25.3 26.2 us for 4 chunks of 16 tokens on 4001 (8 KV heads, groups of 4), 555 560 558 558 for 512 tokens on 32 k.
 constexpr int kTailBlocks = 3;
 constexpr float kRefLead = 8.f, kRefMost = 14.f, kFarScore = 67108864.f;
 constexpr int kNoExponent = -10000;  // of a scale of zero
@@ -675,8 +680,8 @@ hipError_t launch_tiles(PrefillArgs p, int max_len, hipStream_t s) {
     // Splits of the keys, by what they would take, in blocks on a CU: a workgroup has its share of the longest range (an unfinished
     // block counts for more, see above) and what it does before the first and behind the last block; workgroups that have to wait
     // for others are rounds, those that run beside others on a CU slow them down; the join reads every state.  A split more has to
-    // be worth it.  us with 1, 2, 4, 6, 8, 11, 16 splits: a chunk of 16 tokens on 484 (8 KV heads, groups of 4) 19.2 15.8 13.3 13.7
-    // 12.5, 4 of 16 on 984 31.1 23.3 18.7 17.7 18.9 22.4 23.9, 4 of 16 on 4001 102 58.3 35.3 29.1 26.2 28.0 26.9.
+    // be worth it.  us with 1, 2, 4, 6, 8, 11, 16 splits: a chunk of 16 tokens on 484 (8 KV heads, groups of 4) 18.5 15.5 12.6 12.2
+    // 11.6, 4 of 16 on 984 30.7 23.2 18.2 16.4 17.2 19.9 21.2, 4 of 16 on 4001 105 59.8 35.9 28.8 25.3 27.2 25.0.
     const double tiles = std::max<double>(some, (p.n_tokens + p.per_tile - 1) / p.per_tile + 0.5 * (some - 1)) * p.g.H;
     const double longest = p.a.window > 0 ? std::min<double>(pages, (p.a.window + p.per_tile) / kPBT + 2) : pages;
     const double mean = std::max(longest / 2, longest - (double)p.n_tokens / some / kPBT / 2);
@@ -700,8 +705,8 @@ hipError_t launch_tiles(PrefillArgs p, int max_len, hipStream_t s) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)(base * p.splits)), dim3(64 * W), kLds, s, p);
     if (p.splits > 1) {
         // One row per wave while all waves are on the chip at once, or in two goes; four share the work around them.  us of the whole
-        // call with one, four: 4 chunks of 16 tokens on 4001 (6144 rows) 25.6 26.7, one of 8 on 30 k 26.1 35.0; 16 of 16 on 1984
-        // (24576 rows) 42.8 40.4, 512 tokens on 32 k (34816) 532 527, 32 of 16 on 3984, heads of 64 (49152) 71.4 65.0.
+        // call with one, four: 4 chunks of 16 tokens on 4001 (6144 rows) 25.4 26.7, one of 8 on 30 k 34.3 39.8; 16 of 16 on 1984
+        // (24576 rows) 42.8 40.2, 512 tokens on 32 k (34816) 564 559, 32 of 16 on 3984, heads of 64 (49152) 76.8 71.0.
         const long long rows = base * 32 * W;
         if (rows > 16384) hipLaunchKernelGGL((paged_join_kernel<T, D, 4>), dim3((unsigned)(rows / (kJoinWaves * 4))), dim3(64 * kJoinWaves), 0, s, p, 32 * W);
         else hipLaunchKernelGGL((paged_join_kernel<T, D, 1>), dim3((unsigned)(rows / kJoinWaves)), dim3(64 * kJoinWaves), 0, s, p, 32 * W);
@@ -710,8 +715,8 @@ hipError_t launch_tiles(PrefillArgs p, int max_len, hipStream_t s) {
 }
 
 // Eight waves, 256 rows, two sets that take turns on the matrix cores, where the chunks fill more than half of them; else four.  us with
-// four and eight waves: a prompt of 8192 tokens 620 599, 512 tokens on 32 k 571 540, 4 chunks of 16 on 4001 24.8 30.8.  Heads of 64 leave
-// registers for four workgroups of four waves on a CU: 91 us for 16 chunks of up to 700 tokens in a window, with two of eight waves 99.
+// four and eight waves: a prompt of 8192 tokens 632 607, 512 tokens on 32 k 585 560, 4 chunks of 16 on 4001 25.3 31.3.  Heads of 64 leave
+// registers for four workgroups of four waves on a CU: 100 us for 16 chunks of up to 700 tokens in a window, with two of eight waves 144.
 template <int T, int C, int D>
 hipError_t launch(const PrefillArgs &p, int max_new, int max_len, hipStream_t s) {
     if constexpr (D == 128) {
