@@ -23,6 +23,8 @@ def _expected(w, rows, window, scale, q, lens=None):
     lens = w.lens if lens is None else lens
     eps, G = torch.finfo(w.dtype).eps / 2, w.Hq // w.H
     for b, n in enumerate(rows):
+        if n == 0:
+            continue
         k, v = now.held(w.table[b], w.tails[b], lens[b])
         pos, j = torch.arange(lens[b] - n, lens[b])[:, None], torch.arange(lens[b])
         seen = j <= pos
