@@ -361,8 +361,8 @@ kvcomp_status kvcomp_paged_attn_prefill(const kvcomp_paged_config *cfg, const kv
  * append leaves its tail as it was and stores at most those of its whole blocks that have a page, so that it can be repeated
  * with the right table, though not with queries that it has rotated in place; a token at a position outside the table counts as
  * one that holds NaN), Inf or NaN in what was appended (NONFINITE).  The status is that of the first
- * kind, kvcomp_last_error() names all.  SYNCHRONISES `stream` and clears what it reports; what kernels on other streams flag
- * meanwhile is left for the next check. */
+ * kind, kvcomp_last_error() names all.  SYNCHRONISES `stream` and clears the kinds that it reports; others that kernels on other
+ * streams flag meanwhile are left for the next check. */
 kvcomp_status kvcomp_paged_check(const kvcomp_paged_cache *cache, void *stream);
 
 const char *kvcomp_last_error(void);
